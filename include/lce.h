@@ -397,6 +397,136 @@ lce_status_t lce_kd_forward_backward(const lce_kd_problem_t* p,
                                      int32_t* n_valid, int32_t* dev_status, void* dHs, void* dWs,
                                      void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Token embedding: the input end of the [V, D] vocabulary matrix whose output end is the head above
+ * (the same matrix where weights are tied), and its gradient.
+ *
+ *   out[n] = scale * W[id_n]                                         (lookup)
+ *   dW[v]  = scale * sum of dOut[n] over the tokens with id_n = v, id_n != padding_idx
+ *
+ * A vocabulary shard (lce_shard_t's fields: W holds ids [v_begin, v_begin + v) of v_total) looks up
+ * and gathers only its own ids; the outputs of all shards sum to the whole. out and dW are dense.
+ * Elements are bf16 or fp32 (dtype: W, out and dOut; dw_dtype: dW, which may also be fp32 for a bf16
+ * model). Sums run in fp32 in an order that the ids alone fix, and are rounded once.
+ */
+typedef enum lce_dtype {
+  LCE_DTYPE_BF16 = 0,
+  LCE_DTYPE_F32 = 1
+} lce_dtype_t;
+
+#define LCE_NO_PADDING INT64_MIN
+
+/* Bit set in *dev_status by lce_embedding_forward when some id is neither in [0, v_total) nor padding_idx. */
+#define LCE_STATUS_ID_OUT_OF_RANGE 2
+
+typedef struct lce_embedding {
+  int64_t n;                /* tokens, >= 0 and < 2^30 */
+  int64_t d;                /* hidden size (multiple of 8, < 2^20) */
+  int64_t v;                /* rows of W, >= 1 */
+  int64_t ld_w;             /* row stride of W in elements (multiple of 8); 0 means d */
+  int64_t ld_x;             /* row stride of dOut in elements (multiple of 8); 0 means d */
+  int64_t v_begin;          /* first id that W holds */
+  int64_t v_total;          /* ids of the whole vocabulary (< 2^30); 0 means v (and v_begin 0) */
+  int64_t padding_idx;      /* id whose tokens give no gradient, or LCE_NO_PADDING. Inside the vocabulary it
+                               is looked up as any other; outside, its tokens' rows are 0 */
+  float scale;              /* finite */
+  int32_t id_bytes;         /* 4 (int32 ids) or 8 (int64 ids) */
+  int32_t dtype;            /* lce_dtype_t of W, out and dOut */
+  int32_t dw_dtype;         /* lce_dtype_t of dW: dtype, or LCE_DTYPE_F32 */
+  int32_t flags;            /* LCE_FLAG_ACCUMULATE_DW or 0 */
+  int32_t reserved;         /* must be 0 */
+} lce_embedding_t;
+
+/* Workspace bytes of lce_embedding_backward: O(N + V) and fp32 sums of at most 8192 rows of D. */
+lce_status_t lce_embedding_workspace_size(const lce_embedding_t* p, size_t* bwd_bytes);
+
+/*
+ * Lookup (ids need the alignment of their type only). out [N, D], overwritten; the row of an id that W does not hold is 0. dev_status [1] int32
+ * or NULL: overwritten with status bits (LCE_STATUS_ID_OUT_OF_RANGE). p->flags, dw_dtype and ld_x
+ * are checked but not used.
+ */
+lce_status_t lce_embedding_forward(const lce_embedding_t* p, const void* W, const void* ids, void* out,
+                                   int32_t* dev_status, void* stream);
+
+/*
+ * Gradient. dW [V, D] overwritten (rows without a token are 0), or added to with
+ * LCE_FLAG_ACCUMULATE_DW: dW = round(float(dW) + fp32 sum) on the rows that have tokens, and the
+ * others left as they are. With tied weights that adds to what lce_backward wrote.
+ */
+lce_status_t lce_embedding_backward(const lce_embedding_t* p, const void* ids, const void* dOut, void* dW,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One AdamW step over many tensors (a whole model's, or its adapters'), with the arithmetic of
+ * lce_adamw_step element by element: the same bits for bf16 tensors with 32-bit moments. Each tensor is n contiguous elements.
+ *   param          bf16 or fp32, updated in place
+ *   grad           bf16 or fp32, or NULL for a zero gradient
+ *   exp_avg, exp_avg_sq, units: the moments, updated in place (16-byte aligned, units 2). state_bits 32: fp32 [n]
+ *                  each, units NULL. state_bits 8: one byte per element, exp_avg_sq holding the root of
+ *                  the second moment, and two unit bytes for each 32 elements (the last block may be
+ *                  short), [ceil(n / 32)][2]. Zero bytes throughout are the state before the first step.
+ *   master         fp32 [n] or NULL: as W_master of lce_adamw_step, for a bf16 param
+ *   place          8-bit states: where the tensor's elements stand in the call's random numbers
+ *                  (multiple of 32; tensors of one call should not overlap)
+ *   group          index into the hyper-parameters
+ * param, grad and master need the alignment of their element only; 16 bytes is faster.
+ *
+ * 8-bit moments. A block's unit is U = 2^(s - 127) for its byte s (255: the block holds NaN). The byte of
+ * the first moment is a sign and a 7-bit code, that of the root an 8-bit code; code c with k mantissa
+ * bits (3 and 4) stands for q(c) U, q(c) = c below 2^k, else (2^k + c mod 2^k) 2^(floor(c / 2^k) - 1).
+ * U is the power of two that puts the block's largest magnitude into the topmost binade (the next larger
+ * where it would round past the last code), at least 2^-126. Rounding is stochastic: the upper of the two
+ * neighbouring codes with the probability of the value's place between them, so that a moment that moves
+ * by less than a code a step (beta2 near 1) still moves by as much on average. The 16 random bits of an
+ * element come from a hash of (place + index, seed), so a call is deterministic in its arguments. A
+ * nonzero root is held as at least the smallest code. The update itself uses the fp32 moments.
+ *
+ *   grad_scale     device fp32 [1] or NULL: every gradient is multiplied by it first. If it is not finite
+ *                  the call changes nothing (a step with overflowed gradients is skipped on the device).
+ * Tensors with n = 0 are skipped. Tensors must not overlap. count >= 0, n_groups >= 1.
+ */
+typedef struct lce_adamw_tensor {
+  void* param;
+  const void* grad;
+  void* exp_avg;
+  void* exp_avg_sq;
+  void* units;
+  float* master;
+  int64_t n;                /* elements, < 2^35 */
+  int64_t place;
+  int32_t group;
+  int32_t param_dtype;      /* lce_dtype_t */
+  int32_t grad_dtype;       /* lce_dtype_t */
+  int32_t reserved;         /* must be 0 */
+} lce_adamw_tensor_t;
+
+lce_status_t lce_adamw_tensors_step(const lce_adamw_tensor_t* tensors, int64_t count, const lce_adamw_t* groups,
+                                    int32_t n_groups, int32_t state_bits, const float* grad_scale, uint32_t seed,
+                                    void* stream);
+
+/* The values that n 8-bit moments (of one tensor, or of several one after the other in whole blocks) stand
+ * for: the first moment and the root of the second, exactly, as bf16 [n] each. */
+lce_status_t lce_adamw_moments(int64_t n, const void* exp_avg, const void* exp_avg_sq, const void* units,
+                               void* first, void* root, void* stream);
+
+/*
+ * Norm of many gradients together and the factor that clips them (gradient-norm clipping):
+ *   norm   = sqrt(sum over all tensors and elements of g^2)
+ *   factor = min(1, max_norm / (norm + 1e-6)); NaN where the norm is not finite, which
+ *            lce_adamw_tensors_step takes as "skip this step"
+ * norm and factor (may be NULL) are device fp32 [1]. Sums run in fp64. max_norm > 0 (INFINITY: no clipping).
+ */
+typedef struct lce_grad {
+  const void* data;         /* n contiguous elements, aligned to the element; NULL only where n = 0 */
+  int64_t n;                /* < 2^35 */
+  int32_t dtype;            /* lce_dtype_t */
+  int32_t reserved;         /* must be 0 */
+} lce_grad_t;
+
+lce_status_t lce_grad_norm_workspace_size(const lce_grad_t* grads, int64_t count, size_t* bytes);
+lce_status_t lce_grad_norm(const lce_grad_t* grads, int64_t count, float max_norm, float* norm, float* factor,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* lce_status_string(lce_status_t s);
 

@@ -35,6 +35,10 @@ LCE_REDUCE_NONE = 2
 LCE_STATUS_TARGET_OUT_OF_RANGE = 1
 LCE_FLAG_ACCUMULATE_DW = 1
 LCE_FLAG_REUSE_FORWARD = 2
+LCE_DTYPE_BF16 = 0
+LCE_DTYPE_F32 = 1
+LCE_NO_PADDING = -(1 << 63)
+LCE_STATUS_ID_OUT_OF_RANGE = 2
 
 REDUCTIONS = {"mean": LCE_REDUCE_MEAN, "sum": LCE_REDUCE_SUM, "none": LCE_REDUCE_NONE}
 
@@ -45,7 +49,9 @@ EXPORTED = ("lce_workspace_size", "lce_forward", "lce_backward", "lce_status_str
             "lce_combine_shards", "lce_backward_shard", "lce_kd_workspace_size", "lce_kd_forward",
             "lce_kd_backward", "lce_kd_workspace_size_fused", "lce_kd_forward_backward", "lce_plan_info",
             "lce_forward_noalloc", "lce_backward_select", "lce_workspace_size_least",
-            "lce_kd_workspace_size_least")
+            "lce_kd_workspace_size_least", "lce_embedding_workspace_size", "lce_embedding_forward",
+            "lce_embedding_backward", "lce_adamw_tensors_step", "lce_adamw_moments",
+            "lce_grad_norm_workspace_size", "lce_grad_norm")
 
 
 class LceError(RuntimeError):
@@ -92,6 +98,28 @@ class LcePlanInfo(ctypes.Structure):
 
 class LceShard(ctypes.Structure):
     _fields_ = [("v_total", ctypes.c_int64), ("v_begin", ctypes.c_int64)]
+
+
+class LceEmbedding(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int64) for k in ("n", "d", "v", "ld_w", "ld_x", "v_begin", "v_total", "padding_idx")] + [
+        ("scale", ctypes.c_float)] + [(k, ctypes.c_int32) for k in ("id_bytes", "dtype", "dw_dtype", "flags", "reserved")]
+
+
+class LceAdamWTensor(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("param", "grad", "exp_avg", "exp_avg_sq", "units", "master")] + [
+        ("n", ctypes.c_int64), ("place", ctypes.c_int64)] + [
+        (k, ctypes.c_int32) for k in ("group", "param_dtype", "grad_dtype", "reserved")]
+
+
+class LceGrad(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+def embedding(n: int, d: int, v: int, *, ld_w: int = 0, ld_x: int = 0, v_begin: int = 0, v_total: int = 0,
+              padding_idx: int | None = None, scale: float = 1.0, id_bytes: int = 8, dtype: int = LCE_DTYPE_BF16,
+              dw_dtype: int | None = None, flags: int = 0) -> LceEmbedding:
+    return LceEmbedding(n, d, v, ld_w, ld_x, v_begin, v_total, LCE_NO_PADDING if padding_idx is None else padding_idx,
+                        scale, id_bytes, dtype, dtype if dw_dtype is None else dw_dtype, flags, 0)
 
 
 def problem(n: int, d: int, v: int, *, ld_h: int = 0, ld_w: int = 0, ignore_index: int = -100,
@@ -142,6 +170,16 @@ def load() -> ctypes.CDLL:
         lib.lce_kd_forward_backward.argtypes = [KP, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         lib.lce_plan_info.argtypes = [P, ctypes.POINTER(LcePlanInfo)]
         lib.lce_forward_noalloc.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp]
+        E = ctypes.POINTER(LceEmbedding)
+        lib.lce_embedding_workspace_size.argtypes = [E, ctypes.POINTER(sz)]
+        lib.lce_embedding_forward.argtypes = [E, vp, vp, vp, vp, vp]
+        lib.lce_embedding_backward.argtypes = [E, vp, vp, vp, vp, sz, vp]
+        # the tensor tables are passed by address: ctypes arrays of the structures above, or numpy records laid out alike
+        lib.lce_adamw_tensors_step.argtypes = [vp, ctypes.c_int64, vp, ctypes.c_int32, ctypes.c_int32, vp,
+                                               ctypes.c_uint32, vp]
+        lib.lce_adamw_moments.argtypes = [ctypes.c_int64, vp, vp, vp, vp, vp, vp]
+        lib.lce_grad_norm_workspace_size.argtypes = [vp, ctypes.c_int64, ctypes.POINTER(sz)]
+        lib.lce_grad_norm.argtypes = [vp, ctypes.c_int64, ctypes.c_float, vp, vp, vp, sz, vp]
         lib.lce_status_string.argtypes = [ctypes.c_int]
         lib.lce_status_string.restype = ctypes.c_char_p
         lib.lce_timing_enable.argtypes = [ctypes.c_int]
@@ -155,7 +193,9 @@ def load() -> ctypes.CDLL:
                      "lce_forward_shard", "lce_combine_shards", "lce_backward_shard", "lce_kd_workspace_size",
                      "lce_kd_forward", "lce_kd_backward", "lce_kd_workspace_size_fused", "lce_kd_forward_backward",
                      "lce_plan_info", "lce_forward_noalloc", "lce_backward_select", "lce_workspace_size_least",
-                     "lce_kd_workspace_size_least"):
+                     "lce_kd_workspace_size_least", "lce_embedding_workspace_size", "lce_embedding_forward",
+                     "lce_embedding_backward", "lce_adamw_tensors_step", "lce_adamw_moments",
+                     "lce_grad_norm_workspace_size", "lce_grad_norm"):
             getattr(lib, name).restype = ctypes.c_int
         _lib = lib
         return lib
@@ -295,6 +335,45 @@ def lce_kd_forward_backward(p: LceKdProblem, Hs: int, Ws: int, Ht: int, Wt: int,
     _check(load().lce_kd_forward_backward(ctypes.byref(p), Hs, Ws, Ht, Wt, targets, grad_loss, loss, lse_s, lse_t,
                                           n_valid, dev_status or None, dHs, dWs, workspace, workspace_bytes,
                                           stream or None), "lce_kd_forward_backward")
+
+
+def lce_embedding_workspace_size(p: LceEmbedding) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load().lce_embedding_workspace_size(ctypes.byref(p), ctypes.byref(b)), "lce_embedding_workspace_size")
+    return b.value
+
+
+def lce_embedding_forward(p: LceEmbedding, W: int, ids: int, out: int, dev_status: int, stream: int) -> None:
+    _check(load().lce_embedding_forward(ctypes.byref(p), W, ids, out, dev_status or None, stream or None),
+           "lce_embedding_forward")
+
+
+def lce_embedding_backward(p: LceEmbedding, ids: int, dOut: int, dW: int, workspace: int, workspace_bytes: int,
+                           stream: int) -> None:
+    _check(load().lce_embedding_backward(ctypes.byref(p), ids, dOut, dW, workspace, workspace_bytes, stream or None),
+           "lce_embedding_backward")
+
+
+def lce_adamw_tensors_step(tensors: int, count: int, groups: int, n_groups: int, state_bits: int, grad_scale: int,
+                           seed: int, stream: int) -> None:
+    _check(load().lce_adamw_tensors_step(tensors, count, groups, n_groups, state_bits, grad_scale or None, seed,
+                                         stream or None), "lce_adamw_tensors_step")
+
+
+def lce_adamw_moments(n: int, exp_avg: int, exp_avg_sq: int, units: int, first: int, root: int, stream: int) -> None:
+    _check(load().lce_adamw_moments(n, exp_avg, exp_avg_sq, units, first, root, stream or None), "lce_adamw_moments")
+
+
+def lce_grad_norm_workspace_size(grads: int, count: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load().lce_grad_norm_workspace_size(grads, count, ctypes.byref(b)), "lce_grad_norm_workspace_size")
+    return b.value
+
+
+def lce_grad_norm(grads: int, count: int, max_norm: float, norm: int, factor: int, workspace: int,
+                  workspace_bytes: int, stream: int) -> None:
+    _check(load().lce_grad_norm(grads, count, max_norm, norm, factor or None, workspace, workspace_bytes,
+                                stream or None), "lce_grad_norm")
 
 
 def lce_timing_enable(on: bool) -> None:

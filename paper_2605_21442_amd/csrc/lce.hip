@@ -1963,10 +1963,12 @@ __global__ __launch_bounds__(1024) void k_kd_combine(const float* __restrict__ p
 // ---------------------------------------------------------------------------------------------
 enum KernelId { K_COMPACT = 0, K_FWD_STATS, K_COMBINE, K_LOSS, K_GATHER_H, K_BWD_G,
                 K_BWD_DW, K_BWD_DH, K_BWD_DHDW, K_DH_FINAL, K_ADAMW, K_SHARD_COMBINE,
-                K_KD_Z, K_KD_STATS, K_KD_COMBINE, K_KD_P, K_MISC, K_COUNT };
+                K_KD_Z, K_KD_STATS, K_KD_COMBINE, K_KD_P, K_EMBED_LOOKUP, K_EMBED_SORT, K_EMBED_GRAD,
+                K_ADAMW_TENSORS, K_ADAMW_MOMENTS, K_GRAD_NORM, K_MISC, K_COUNT };
 const char* const kKernelNames[K_COUNT] = {"compact", "fwd_stats", "combine", "loss", "gather_h", "bwd_g",
                                            "bwd_dw", "bwd_dh", "bwd_dhdw", "dh_finalize", "adamw", "shard_combine",
-                                           "kd_teacher_z", "kd_student_stats", "kd_combine", "kd_teacher_p", "misc"};
+                                           "kd_teacher_z", "kd_student_stats", "kd_combine", "kd_teacher_p", "embed_lookup",
+                                           "embed_sort", "embed_grad", "adamw_tensors", "adamw_moments", "grad_norm", "misc"};
 
 struct Timing {
   std::mutex mu;
@@ -3006,3 +3008,7 @@ lce_status_t lce_timing_read(int k, double* total_ms, int64_t* launches) {
 }
 
 }  // extern "C"
+
+// the other operators of a training step: token embedding, AdamW over many tensors, gradient norm
+#include "embedding.h"
+#include "optimizer.h"

@@ -1,0 +1,428 @@
+"""AdamW over many tensors, its 8-bit moments, and the gradient norm.
+
+* 32-bit moments: bit for bit the single-matrix step (lce_adamw_step) on bf16 tensors, the float64 oracle on fp32;
+* 8-bit moments: the codes of the float64 update, except where fp32 rounding moves a value across the border between
+  two codes (the borders' width is counted), and the parameters of the float64 update;
+* the norm against float64: fp64 sums, so off by its last rounding to fp32 (2^-24)."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+from oracle import adamw_oracle as AO
+from oracle import training_oracle as T
+
+pytestmark = pytest.mark.gpu
+
+F32 = lambda x: float(np.float32(x))
+HP = dict(lr=F32(1e-3), betas=(F32(0.9), F32(0.95)), eps=F32(1e-8), weight_decay=F32(0.1))
+
+
+def _o(step, **kw):
+    hp = {**HP, **kw}
+    return dict(lr=hp["lr"], beta1=hp["betas"][0], beta2=hp["betas"][1], eps=hp["eps"], weight_decay=hp["weight_decay"], step=step)
+
+
+def _draw(shape, seed, std=1.0, dtype=None):
+    import torch
+    g = torch.Generator(device="cuda:0").manual_seed(seed)
+    return (std * torch.randn(shape, device="cuda:0", generator=g)).to(dtype or torch.float32)
+
+
+def _np(x):
+    return x.detach().double().cpu().numpy().reshape(-1)
+
+
+SHAPES = [(1,), (31,), (32,), (33,), (7, 9), (264, 40), (5000,), (4097,), (0,), (3, 8, 8)]
+
+
+@pytest.mark.parametrize("master", [False, True])
+def test_bf16_tensors_take_the_bits_of_the_single_step(master):
+    import torch
+    from paper_2605_21442_amd import AdamWState, AdamWTensors
+    shapes = [(300, 264), (1, 8), (1000, 72), (513, 8)]
+    ws = [_draw(s, k, 0.02, torch.bfloat16) for k, s in enumerate(shapes)]
+    ref = [w.clone() for w in ws]
+    many = AdamWTensors(ws, master_weights=master, **HP)
+    one = [AdamWState(w, lr=HP["lr"], betas=HP["betas"], eps=HP["eps"], weight_decay=HP["weight_decay"], master_weights=master)
+           for w in ref]
+    for t in range(3):
+        gs = [_draw(s, 10 * t + k, 0.01, torch.bfloat16) for k, s in enumerate(shapes)]
+        many.step(gs)
+        for st, g in zip(one, gs):
+            st.step_with(g)
+        for k, st in enumerate(one):
+            o, n = many.offsets[k], ws[k].numel()
+            assert torch.equal(ws[k], ref[k])
+            assert torch.equal(many.exp_avg[o:o + n], st.exp_avg.reshape(-1))
+            assert torch.equal(many.exp_avg_sq[o:o + n], st.exp_avg_sq.reshape(-1))
+            if master:
+                assert torch.equal(many.master[o:o + n], st.master.reshape(-1))
+
+
+@pytest.mark.parametrize("pdt,gdt", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32")])
+def test_types_odd_sizes_and_groups_match_the_oracle(pdt, gdt):
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}
+    ps = [_draw(s, k, 0.5, dt[pdt]) for k, s in enumerate(SHAPES)]
+    opt = AdamWTensors([dict(params=ps[:4]), dict(params=ps[4:], lr=F32(3e-3), weight_decay=0.0, betas=(F32(0.8), F32(0.99)))], **HP)
+    scale = torch.tensor(0.375, device="cuda:0")
+    theta = [_np(p) for p in ps]
+    m, v = [np.zeros(p.numel()) for p in ps], [np.zeros(p.numel()) for p in ps]
+    mag = [np.zeros(p.numel()) for p in ps]        # the first moment's terms may cancel: their magnitudes
+    for t in (1, 2, 3):
+        gs = [_draw(s, 20 * t + k, 0.1, dt[gdt]) for k, s in enumerate(SHAPES)]
+        opt.step(gs, grad_scale=scale)
+        for k in range(len(ps)):
+            kw = {} if k < 4 else dict(lr=F32(3e-3), weight_decay=0.0, betas=(F32(0.8), F32(0.99)))
+            if pdt == "bf16":
+                theta[k] = before[k] if t > 1 else theta[k]
+            theta[k], m[k], v[k] = AO.adamw_step(theta[k], 0.375 * _np(gs[k]), m[k], v[k], **_o(t, **kw))
+            o, n = opt.offsets[k], ps[k].numel()
+            # a step rounds the scaled gradient, two products and their sum: 2^-24 each of terms no larger than mag, which
+            # decays no faster than the errors of earlier steps do
+            beta1 = kw.get("betas", HP["betas"])[0]
+            mag[k] = beta1 * mag[k] + (1 - beta1) * 0.375 * np.abs(_np(gs[k]))
+            assert np.all(np.abs(_np(opt.exp_avg[o:o + n]) - m[k]) <= 4 * t * 2.0 ** -24 * mag[k] + 1e-30)
+            np.testing.assert_allclose(_np(opt.exp_avg_sq[o:o + n]), v[k], rtol=1e-6, atol=1e-15)
+            tol = 1e-6 * np.abs(theta[k]) + 1e-5 * 3e-3 + (2.0 ** -8 * np.abs(theta[k]) if pdt == "bf16" else 0)
+            assert np.all(np.abs(_np(ps[k]) - theta[k]) <= tol), k
+        before = [_np(p) for p in ps]
+
+
+def _codes(opt, k):
+    o, n = opt.offsets[k], opt.params[k].numel()
+    s = opt.units[o // 32:(o + n + 31) // 32].long().cpu().numpy()
+    s = np.repeat(s, 32, axis=0)[:n]
+    cm, cr = (x[o:o + n].long().cpu().numpy() for x in (opt.exp_avg, opt.exp_avg_root))
+    return cm, cr, s[:, 0], s[:, 1]
+
+
+@pytest.mark.parametrize("pdt,master", [("f32", False), ("bf16", False), ("bf16", True)])
+def test_8_bit_step_matches_the_oracle(pdt, master):
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[pdt]
+    ps = [_draw(s, k, 0.5, dt) for k, s in enumerate(SHAPES)]
+    opt = AdamWTensors(ps, master_weights=master, state_bits=8, **HP)
+    m, v = [np.zeros(p.numel()) for p in ps], [np.zeros(p.numel()) for p in ps]
+    crossed = total = 0
+    for t in (1, 2, 3, 4):
+        # magnitudes over six decades within a block, zeros among them
+        gs = [(_draw(s, 30 * t + k) * 10.0 ** (3 * _draw(s, 90 * t + k)).clamp(-6, 0)) for k, s in enumerate(SHAPES)]
+        for g in gs:
+            g[..., ::5] = 0
+        start = [_np(p) if not master else _np(opt.master[o:o + p.numel()]) for p, o in zip(ps, opt.offsets)]
+        opt.step(gs, seed=1000 + t)
+        first, root = opt.moments()
+        for k, p in enumerate(ps):
+            o, n = opt.offsets[k], p.numel()
+            if n == 0:
+                continue
+            g = _np(gs[k])
+            mag = HP["betas"][0] * np.abs(m[k]) + (1 - HP["betas"][0]) * np.abs(g)
+            theta, m1, v1 = AO.adamw_step(start[k], g, m[k], v[k], **_o(t))
+            now = _np(opt.master[o:o + n]) if master else _np(p)
+            tol = 1e-6 * np.abs(theta) + 1e-5 * HP["lr"]
+            assert np.all(np.abs(now - theta) <= tol + (2.0 ** -8 * (np.abs(theta) + tol) if pdt == "bf16" and not master else 0)), (t, k)
+            u = T.pair_uniform(o, n, 1000 + t)
+            cm, cr, sm, sr = _codes(opt, k)
+            assert np.array_equal(sm, np.repeat(T.units(m1, 3), 32)[:n]) and np.array_equal(sr, np.repeat(T.units(np.sqrt(v1), 4), 32)[:n])
+            for x, err, c, s, mant in [(m1, 4 * 2.0 ** -24 * mag, cm & 127, sm, 3),
+                                       (np.sqrt(v1), 4 * 2.0 ** -24 * np.sqrt(v1), cr, sr, 4)]:
+                at, size = T.place_between(x, s, mant)
+                d = err / size + 2.0 ** -18                  # fp32 error of the value; of the sum with u (below 32)
+                low, high = np.floor(at - d + u), np.floor(at + d + u)
+                if mant == 4:
+                    low, high = (np.maximum(z, (x > 0).astype(float)) for z in (low, high))
+                assert np.all((c >= low) & (c <= high)), (t, k, mant)
+                crossed += int(np.sum(low != high))
+                total += n
+            assert np.all(((cm >> 7) == 1) == (np.signbit(m1))[:n])
+            # the state stands for these values, from which the next step starts; bf16 holds them exactly
+            m[k] = np.where(cm > 127, -1, 1) * T.value(cm & 127, sm, 3)
+            r = T.value(cr, sr, 4)
+            assert np.array_equal(_np(first[o:o + n]), m[k]) and np.array_equal(_np(root[o:o + n]), r)
+            v[k] = r ** 2
+    assert crossed <= 1e-3 * total                           # so the comparison says something
+
+
+def test_8_bit_moments_follow_a_constant_gradient_on_average():
+    # both moments move by less than a code a step at the end (beta2 = 0.999): nearest rounding would stop them
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    n, steps, b1, b2 = 1 << 15, 400, 0.9, 0.999
+    p = torch.zeros(n, device="cuda:0")
+    g = _draw(n, 70).abs() * 0.1 + 0.01
+    opt = AdamWTensors([p], lr=0.0, betas=(b1, b2), state_bits=8, seed=3)
+    for _ in range(steps):
+        opt.step([g])
+    first, root = opt.moments()
+    # a step's rounding is off by less than 1/8 (first) and 1/16 (root) of the value with mean 0, so with variance at
+    # most p (1 - p) of that squared; sums over the moments' memory, then the mean over n elements: below 1 %
+    rm = float((first.double() / g.double()).mean()) / (1 - b1 ** steps)
+    rv = float((root.double() / g.double()).mean()) / math.sqrt(1 - b2 ** steps)
+    assert abs(rm - 1) < 0.01 and abs(rv - 1) < 0.02, (rm, rv)
+    before = float(root.double().mean())
+    for _ in range(300):
+        opt.step([torch.zeros_like(g)])
+    after = float(opt.moments()[1].double().mean())
+    assert abs(after / before / b2 ** 150 - 1) < 0.02, (after, before)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_views_at_any_alignment_and_many_tensors(bits):
+    # 200 tensors (several launches), parameters and gradients at odd places of flat buffers, in 20 groups
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    rng = np.random.default_rng(5)
+    sizes = [int(x) for x in rng.integers(1, 3000, 200)]
+    offs = np.concatenate([[1], 1 + np.cumsum(sizes)])
+    flat, gflat = _draw(int(offs[-1]) + 8, 80, 0.5, torch.bfloat16), _draw(int(offs[-1]) + 8, 81, 0.1, torch.bfloat16)
+    keep, views = flat.clone(), lambda x: [x[int(o):int(o) + s] for o, s in zip(offs, sizes)]
+    groups = lambda ps: [dict(params=ps[10 * k:10 * k + 10], lr=F32(1e-3 * (k + 1))) for k in range(20)]
+    opt = AdamWTensors(groups(views(flat)), betas=HP["betas"], state_bits=bits, seed=9)
+    apart = [x.clone() for x in views(keep)]
+    ref = AdamWTensors(groups(apart), betas=HP["betas"], state_bits=bits, seed=9)
+    for _ in range(2):
+        opt.step(views(gflat))
+        ref.step([x.clone() for x in views(gflat)])
+    for a, b in zip(views(flat), apart):
+        assert torch.equal(a, b)
+    assert torch.equal(opt.exp_avg, ref.exp_avg)
+    assert torch.equal(flat[:1], keep[:1]) and torch.equal(flat[int(offs[-1]):], keep[int(offs[-1]):])   # around them
+    # each group has its own rate: the first step moves every element by about it
+    x = AdamWTensors([dict(params=[torch.zeros(64, device="cuda:0")], lr=F32(0.01 * (k + 1))) for k in range(20)], weight_decay=0.0)
+    x.step([torch.ones(64, device="cuda:0")] * 20)
+    for k, p in enumerate(x.params):
+        assert torch.allclose(p, torch.full_like(p, -0.01 * (k + 1)), rtol=1e-5)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_missing_gradients_and_skipped_steps_leave_everything(bits):
+    import torch
+    from paper_2605_21442_amd import AdamWTensors, grad_norm
+    ps = [_draw(100, k) for k in range(3)]
+    opt = AdamWTensors(ps, state_bits=bits, **HP)
+    gs = [_draw(100, 5 + k) for k in range(3)]
+    opt.step(gs)
+    all_of = lambda: [x.clone() for x in ps + [v for v in opt.state_dict().values() if isinstance(v, torch.Tensor)]]
+    before = all_of()
+    opt.step([gs[0], None, gs[2]])
+    o = opt.offsets[1]
+    assert torch.equal(ps[1], before[1]) and not torch.equal(ps[0], before[0])
+    assert torch.equal(opt.exp_avg[o:o + 100], before[3][o:o + 100])
+    before = all_of()
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        opt.step(gs, grad_scale=torch.tensor(bad, device="cuda:0"))
+    gs[1][7] = float("inf")
+    norm, factor = grad_norm(gs, 1.0)
+    assert norm.item() == float("inf") and math.isnan(factor.item())
+    opt.step(gs, grad_scale=factor)
+    assert all(torch.equal(a, b) for a, b in zip(before, all_of()))
+    assert opt.step_count == 6
+    opt.step([None, None, None])
+    assert all(torch.equal(a, b) for a, b in zip(before, all_of()))
+
+
+def test_a_nan_gradient_stays_in_its_block():
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    p = _draw(100, 1)
+    opt = AdamWTensors([p], state_bits=8, **HP)
+    g = _draw(100, 2)
+    g[40], g[70] = float("nan"), float("inf")
+    opt.step([g])
+    first, root = opt.moments()
+    bad = torch.zeros(128, dtype=torch.bool, device="cuda:0")
+    bad[32:96] = True                                  # the blocks of elements 40 and 70
+    assert torch.equal(first.isnan(), bad) and torch.equal(root.isnan(), bad)
+    assert torch.isfinite(p[:32]).all() and torch.isfinite(p[96:]).all() and p[40].isnan()
+    opt.step([_draw(100, 3)])
+    assert torch.equal(opt.moments()[0].isnan(), bad)
+
+
+def test_extreme_magnitudes_in_8_bits():
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    p = torch.zeros(96, device="cuda:0")
+    opt = AdamWTensors([p], state_bits=8, betas=(F32(0.9), F32(0.95)), lr=1e-3, weight_decay=0.0)
+    g = torch.zeros(96, device="cuda:0")
+    g[0], g[33], g[64], g[65] = 1e18, 1e-30, 1e-44, -1e-15
+    opt.step([g])
+    first, root = opt.moments()
+    m = 0.1 * g.double()
+    for i in (0, 65):
+        assert abs(float(first[i]) - float(m[i])) <= abs(float(m[i])) / 8
+    assert abs(float(first[33]) - 1e-31) <= 1.25e-32 and float(root[33]) == 0         # g^2 is below fp32
+    assert not first[1:32].any() and torch.isfinite(first).all() and torch.isfinite(root).all()
+
+
+def test_state_round_trip_continues_bit_for_bit():
+    import copy
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    for bits in (32, 8):
+        p = [_draw(s, k, 0.5, torch.bfloat16) for k, s in enumerate(SHAPES)]
+        a = AdamWTensors(p, state_bits=bits, master_weights=True, seed=5, **HP)
+        gs = [[_draw(s, 10 * t + k, 0.1, torch.bfloat16) for k, s in enumerate(SHAPES)] for t in range(4)]
+        for g in gs[:2]:
+            a.step(g)
+        q = [x.clone() for x in p]
+        b = AdamWTensors(q, state_bits=bits, master_weights=True)
+        b.load_state_dict(copy.deepcopy(a.state_dict()))
+        for g in gs[2:]:
+            a.step(g)
+            b.step(g)
+        assert all(torch.equal(x, y) for x, y in zip(p, q)) and torch.equal(a.exp_avg, b.exp_avg) and a.step_count == b.step_count
+        with pytest.raises(ValueError):
+            AdamWTensors(q, state_bits=40 - bits, master_weights=True).load_state_dict(a.state_dict())
+        with pytest.raises(ValueError):
+            AdamWTensors(q, state_bits=bits).load_state_dict(a.state_dict())
+        with pytest.raises(ValueError):
+            AdamWTensors(q[:-1], state_bits=bits, master_weights=True).load_state_dict(a.state_dict())
+
+
+def test_refusals():
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    p = _draw((8, 8), 1)
+    with pytest.raises(ValueError, match="overlap"):
+        AdamWTensors([p, p])
+    with pytest.raises(ValueError, match="overlap"):
+        AdamWTensors([p.view(-1)[:40], p.view(-1)[39:]])
+    with pytest.raises(ValueError):
+        AdamWTensors([p.T])
+    opt = AdamWTensors([p, _draw(5, 2)], **HP)
+    g = [_draw((8, 8), 3), _draw(5, 4)]
+    for bad, err in [([g[0]], ValueError), ([g[0], g[0]], ValueError), ([g[0].view(64), g[1]], ValueError),
+                     ([g[0].half(), g[1]], TypeError), ([g[0].cpu(), g[1]], ValueError)]:
+        with pytest.raises(err):
+            opt.step(bad)
+    for scale in (torch.ones(2, device="cuda:0"), torch.ones(1), torch.ones(1, device="cuda:0", dtype=torch.float64)):
+        with pytest.raises(ValueError):
+            opt.step(g, grad_scale=scale)
+    assert opt.step_count == 0
+    with pytest.raises(ValueError):
+        opt.moments()
+    q = opt.params[1]
+    q.data = q.clone()
+    with pytest.raises(ValueError, match="storage"):
+        opt.step(g)
+    r = AdamWTensors([p], **HP)
+    before = p.clone()
+    r.step([g[0].T.contiguous().T])                    # a strided gradient is copied
+    s = AdamWTensors([before], **HP)
+    s.step([g[0]])
+    assert torch.equal(p, before)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_norm_matches_float64(dt):
+    import torch
+    from paper_2605_21442_amd import grad_norm
+    dtype = {"bf16": torch.bfloat16, "f32": torch.float32}[dt]
+    for sizes in ([1], [7, 1, 3], [5000, 0, 77], [1 << 20, 3], [int(x) for x in np.random.default_rng(1).integers(1, 40000, 400)]):
+        flat = _draw(sum(sizes) + 1, 3, 0.3, dtype)
+        offs = np.concatenate([[1], 1 + np.cumsum(sizes)])                # odd alignments
+        gs = [flat[int(o):int(o) + s] for o, s in zip(offs, sizes)]
+        ref, _ = T.norm([_np(g) for g in gs])
+        for most in (math.inf, F32(2 * ref), F32(0.25 * ref)):
+            norm, factor = grad_norm(gs, most)
+            assert norm.shape == () and abs(norm.item() - ref) <= ref * 2.0 ** -24 * 1.001
+            f = min(1.0, most / (ref + 1e-6))
+            assert abs(factor.item() - f) <= f * 2.0 ** -24 * 1.001
+        assert [x.item() for x in grad_norm(gs, F32(0.25 * ref))] == [norm.item(), factor.item()]     # the same bits
+
+
+def test_norm_of_large_small_and_no_values():
+    import torch
+    from paper_2605_21442_amd import grad_norm
+    big = torch.full((4,), 3e38, dtype=torch.bfloat16, device="cuda:0")
+    assert abs(grad_norm([big[:1]])[0].item() / float(big[0]) - 1) < 1e-6              # its square is beyond fp32
+    assert grad_norm([big])[0].item() == float("inf") and math.isnan(grad_norm([big], 1.0)[1].item())
+    tiny = torch.full((100,), 1e-30, device="cuda:0")
+    assert abs(grad_norm([tiny])[0].item() / 1e-29 - 1) < 1e-6                         # and these are below it
+    zero = torch.zeros(10, device="cuda:0")
+    norm, factor = grad_norm([zero, None, zero[:0]], 1.0)
+    assert norm.item() == 0 and factor.item() == 1
+    nan = torch.tensor([1.0, float("nan")], device="cuda:0")
+    norm, factor = grad_norm([zero, nan], 1.0)
+    assert math.isnan(norm.item()) and math.isnan(factor.item())
+
+
+def _step_of_a_small_model():
+    """ids -> embedding -> two matrices -> loss -> gradients -> clipped AdamW, weights tied; returns a function that runs one
+    step, what it changes, and the optimizer."""
+    import torch
+    from paper_2605_21442_amd import AdamWTensors, autograd as AG, grad_norm, token_embedding
+    from paper_2605_21442_amd.training import embedding_backward
+    n, d, v = 256, 64, 300
+    w, a = _draw((v, d), 1, 0.2, torch.bfloat16), _draw((d, d), 2, 0.1, torch.bfloat16)
+    ids = torch.from_numpy(np.random.default_rng(3).integers(0, v, n + 1)).to("cuda:0")
+    opt = AdamWTensors([dict(params=[w]), dict(params=[a], weight_decay=0.0)], master_weights=True, state_bits=8, **HP)
+    one = torch.ones(1, device="cuda:0")
+
+    def step():
+        x = token_embedding(ids[:-1], w, scale=8.0)
+        h = x + x @ a
+        loss, lse, nv, _, ws = AG.forward(h, w, ids[1:], keep_workspace=True)
+        dh, dw = AG.backward(h, w, ids[1:], lse, nv, one, workspace=ws)
+        da, dx = x.T @ dh, dh + dh @ a.T
+        embedding_backward(ids[:-1], dx, v, 8.0, accumulate_into=dw)
+        norm, factor = grad_norm([dw, da], 0.5)
+        opt.step([dw, da], grad_scale=factor, seed=77)
+        return loss, norm
+    return step, [w, a, opt.exp_avg, opt.exp_avg_root, opt.units, opt.master], opt
+
+
+def test_a_captured_training_step_replays_like_eager_steps():
+    import torch
+    eager, state, opt = _step_of_a_small_model()
+    eager()                                         # warm-up (the library products' workspaces)
+    torch.cuda.synchronize()
+    start = [x.clone() for x in state]
+    captured, own, _ = _step_of_a_small_model()
+    captured()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss, norm = captured()
+    for rep in range(3):
+        # both from the same state; the captured step's bias correction is the step count at its capture, 2
+        for x, y, s in zip(own, state, start):
+            x.copy_(s)
+            y.copy_(s)
+        opt.step_count = 1
+        ref_loss, ref_norm = eager()
+        _ = torch.randn(512, 512, device="cuda:0").square().sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert loss.item() == ref_loss.item() and norm.item() == ref_norm.item()
+        assert all(torch.equal(x, y) for x, y in zip(own, state))
+        start = [x.clone() for x in state]
+
+
+def test_two_states_on_two_streams():
+    import torch
+    from paper_2605_21442_amd import AdamWTensors, grad_norm
+    make = lambda: [_draw(50000, k) for k in range(4)]
+    gs = [_draw(50000, 10 + k) for k in range(4)]
+    ref = make()
+    opt = AdamWTensors(ref, **HP)
+    for _ in range(3):
+        opt.step(gs, grad_scale=grad_norm(gs, 1.0)[1])
+    torch.cuda.synchronize()
+    sets = [make(), make()]
+    opts = [AdamWTensors(s, **HP) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for s, o in zip(streams, opts):
+            with torch.cuda.stream(s):
+                o.step(gs, grad_scale=grad_norm(gs, 1.0)[1])
+    torch.cuda.synchronize()
+    for ps in sets:
+        assert all(torch.equal(a, b) for a, b in zip(ps, ref))
