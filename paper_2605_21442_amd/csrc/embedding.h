@@ -2,7 +2,8 @@
 //
 // The gradient adds each id's tokens in an order that the ids alone fix, without atomics on sums:
 //   sort: tokens grouped by id, in token order within an id (a stable counting sort, one launch);
-//   grad: per id the fp32 sum of its tokens' rows of dOut, scaled, rounded and stored (or added).
+//   grad: the fp32 sums of the rows of dOut by runs of sorted tokens, and the rows without tokens;
+//   join: the sums of the ids that several runs share.
 #pragma once
 
 namespace {
@@ -17,42 +18,56 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 constexpr int kSortWaves = 16;
 constexpr int kSortIds = 512;      // most ids of a bucket
-constexpr int kSortAhead = 8;      // loads in flight per lane
+constexpr int kSortAhead = 8;      // groups of 64 tokens whose ids a wave loads ahead
 
-struct EmbedIds {
+// rows of W that get a gradient: id - v_begin in [0, v), other than the padding id's (pad_row, or -1)
+struct EmbedRows {
   const void* ids;
-  int bytes;
-  int64_t n, v_begin, v, padding;
+  int64_t n, v_begin;
+  uint32_t v;
+  int pad_row;
 };
 
-// the row of token i's id in this shard, or -1
-__device__ __forceinline__ int embed_row(const EmbedIds& e, int64_t i) {
-  if (i >= e.n) return -1;
-  const int64_t id = load_target(e.ids, e.bytes, i);
-  const int64_t r = id - e.v_begin;
-  return id != e.padding && id >= e.v_begin && r < e.v ? (int)r : -1;
+// the row of token i's id and its bucket, INT_MAX where the token has none
+template <int kBytes>
+__device__ __forceinline__ int embed_bucket(const EmbedRows& e, int64_t i, int64_t i1, int mask, int* row) {
+  bool ok = i < i1;
+  uint32_t r = 0;
+  if (kBytes == 8) {
+    const uint64_t u = ok ? (uint64_t)(((const int64_t*)e.ids)[i] - e.v_begin) : 0;
+    ok &= u < e.v;
+    r = (uint32_t)u;
+  } else {
+    r = ok ? ((const uint32_t*)e.ids)[i] - (uint32_t)e.v_begin : 0;   // (v_begin + v <= 2^30: no id wraps into the rows)
+    ok &= r < e.v;
+  }
+  *row = (int)r;
+  return ok && (int)r != e.pad_row ? (int)(r & mask) : 0x7FFFFFFF;
 }
 
-__global__ __launch_bounds__(1024) void k_embed_sort(EmbedIds e, int nb_log2, int rows, int2* __restrict__ sorted,
+template <int kBytes>
+__global__ __launch_bounds__(1024) void k_embed_sort(EmbedRows e, int nb_log2, int rows, int2* __restrict__ sorted,
                                                      int* __restrict__ starts) {
   __shared__ int cnt[kSortIds * kSortWaves];   // [id of the bucket][wave]: count, then place of the next token
   __shared__ int wsum[kSortWaves], below_all[kSortWaves];
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  const int nb_mask = (1 << nb_log2) - 1, b = blockIdx.x;
+  const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int mask = (1 << nb_log2) - 1, b = blockIdx.x;
   for (int i = t; i < rows * kSortWaves; i += 1024) cnt[i] = 0;
   __syncthreads();
   const int64_t per = (e.n + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
   const int64_t i0 = w * per, i1 = min(e.n, i0 + per);
   int below = 0;
-  for (int64_t i = i0; i < i1; i += 64 * kSortAhead) {
-    int r[kSortAhead];
+  unsigned long long hits = 0;       // bit g: the wave's groups g, g + 64, ... hold tokens of the bucket
+  int g = 0;
+  for (int64_t i = i0; i < i1; i += 64 * kSortAhead, g += kSortAhead) {
+    int r[kSortAhead], rb[kSortAhead];
 #pragma unroll
-    for (int k = 0; k < kSortAhead; ++k) r[k] = i + 64 * k < i1 ? embed_row(e, i + 64 * k + lane) : -1;
+    for (int k = 0; k < kSortAhead; ++k) rb[k] = embed_bucket<kBytes>(e, i + 64 * k + lane, i1, mask, &r[k]);
 #pragma unroll
     for (int k = 0; k < kSortAhead; ++k) {
-      const int rb = r[k] & nb_mask;
-      below += r[k] >= 0 && rb < b;
-      if (r[k] >= 0 && rb == b) atomicAdd(&cnt[(r[k] >> nb_log2) * kSortWaves + w], 1);
+      below += rb[k] < b;
+      if (rb[k] == b) atomicAdd(&cnt[(r[k] >> nb_log2) * kSortWaves + w], 1);
+      hits |= (unsigned long long)(__ballot(rb[k] == b) != 0) << ((g + k) & 63);
     }
   }
   for (int m = 32; m >= 1; m >>= 1) below += __shfl_xor(below, m);
@@ -87,28 +102,44 @@ __global__ __launch_bounds__(1024) void k_embed_sort(EmbedIds e, int nb_log2, in
     }
     at += own[k];
   }
-  if (b == nb_mask && t == 1023) starts[((int64_t)nb_mask + 1) * rows] = at;
+  if (b == mask && t == 1023) starts[((int64_t)mask + 1) * rows] = at;
   __syncthreads();
-  for (int64_t i = i0; i < i1; i += 64 * kSortAhead) {
-    int r[kSortAhead];
+  g = 0;
+  for (int64_t i = i0; i < i1; i += 64 * kSortAhead, g += kSortAhead) {
+    if (((hits >> (g & 63)) & ((1u << kSortAhead) - 1)) == 0) continue;
+    int r[kSortAhead], rb[kSortAhead];
 #pragma unroll
-    for (int k = 0; k < kSortAhead; ++k) r[k] = i + 64 * k < i1 ? embed_row(e, i + 64 * k + lane) : -1;
+    for (int k = 0; k < kSortAhead; ++k) rb[k] = embed_bucket<kBytes>(e, i + 64 * k + lane, i1, mask, &r[k]);
 #pragma unroll
     for (int k = 0; k < kSortAhead; ++k) {
-      const bool in = r[k] >= 0 && (r[k] & nb_mask) == b;
-      unsigned long long same = __ballot(in);
-      if (same == 0) continue;
-      const int q = in ? r[k] >> nb_log2 : 0;
-      // the lanes with this lane's id, from one ballot per bit of it
+      unsigned long long todo = __ballot(rb[k] == b);
+      if (todo == 0) continue;
+      const int q = r[k] >> nb_log2;
+      const int2 pair = make_int2(r[k], (int)(i + 64 * k + lane));
+      // the lanes of one id after the other, for the first few ids (a group has 64 / nb of a bucket's tokens on
+      // average, besides a frequent id's) ...
+      for (int few = 0; todo && few < 3; ++few) {
+        const int q1 = __builtin_amdgcn_readlane(q, __builtin_ctzll(todo));
+        const unsigned long long same = __ballot(rb[k] == b && q == q1);
+        volatile int* place = &cnt[q1 * kSortWaves + w];   // this wave's own entries
+        const int p = *place;
+        if (rb[k] == b && q == q1) sorted[p + __popcll(same & ((1ull << lane) - 1ull))] = pair;
+        if (lane == 0) *place = p + __popcll(same);
+        todo &= ~same;
+      }
+      if (todo == 0) continue;
+      // ... and all others at once: the lanes with this lane's id, from one ballot per bit of it
+      const bool in = (todo >> lane) & 1;
+      unsigned long long same = todo;
       for (int bit = 0; (rows - 1) >> bit; ++bit) {
         const unsigned long long m = __ballot((q >> bit) & 1);
         same &= (q >> bit) & 1 ? m : ~m;
       }
+      volatile int* place = &cnt[(in ? q : 0) * kSortWaves + w];
       const int rank = __popcll(same & ((1ull << lane) - 1ull));
-      volatile int* place = &cnt[q * kSortWaves + w];   // this wave's own entries
-      const int p = in ? *place + rank : 0;
+      const int p = *place + rank;
       if (in && rank == 0) *place = p + __popcll(same);
-      if (in) sorted[p] = make_int2(r[k], (int)(i + 64 * k + lane));
+      if (in) sorted[p] = pair;
     }
   }
 }
@@ -145,6 +176,12 @@ template <> struct Row8<float> {
   }
 };
 
+struct EmbedIds {
+  const void* ids;
+  int bytes;
+  int64_t n, v_begin, v, padding;
+};
+
 template <typename T>
 __global__ __launch_bounds__(256) void k_embed_lookup(EmbedIds e, int64_t v_total, const T* __restrict__ W, int64_t ldw,
                                                       int d, float scale, T* __restrict__ out, int* status) {
@@ -170,32 +207,134 @@ __global__ __launch_bounds__(256) void k_embed_lookup(EmbedIds e, int64_t v_tota
 __global__ void k_embed_clear_status(int* status) { *status = 0; }
 
 // ---------------------------------------------------------------------------------------------
-// Gradient: one workgroup per id.
+// Gradient: the sorted tokens are cut into chunks of `per` consecutive ones, and a wave takes a chunk's tokens at
+// 512 columns (8 per lane), eight rows of dOut in flight. An id whose tokens lie in one chunk is finished there. One
+// that reaches over a chunk's edge leaves an fp32 sum per chunk, in the chunk's slot 0 where it goes on from the chunk
+// before and in slot 1 where it starts, and k_embed_join adds these in the order of the chunks. So a frequent id
+// is spread over many waves, and the order of all sums follows from the ids and N alone.
+// Behind the chunks the same launch zeroes the rows of a fresh dW that have no token.
 // ---------------------------------------------------------------------------------------------
+constexpr int kGradCols = 512;     // columns of a wave
+constexpr int kFillRows = 16;      // ids whose rows a wave zeroes, where they have no token
+
+struct EmbedSorted {
+  const int2* pairs;               // (row of W, token), by id
+  const int* starts;               // first pair of each id, bucket by bucket
+  int nb_log2, rows;
+  __device__ __forceinline__ int64_t slot(int r) const { return (int64_t)(r & ((1 << nb_log2) - 1)) * rows + (r >> nb_log2); }
+  __device__ __forceinline__ int count() const { return starts[(int64_t)rows << nb_log2]; }
+};
+
+template <typename TW, bool kAdd>
+__device__ __forceinline__ void grad_store(TW* o, const float sum[8], float scale) {
+  float x[8] = {};
+  if (kAdd) Row8<TW>::load(o, x);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x[k] += scale * sum[k];
+  Row8<TW>::store(o, x);
+}
+
 template <typename T, typename TW, bool kAdd>
-__global__ __launch_bounds__(256) void k_embed_grad(const int2* __restrict__ sorted, const int* __restrict__ starts,
-                                                    int nb_log2, int rows, int v, const T* __restrict__ dout, int64_t ldx, int d,
-                                                    float scale, TW* __restrict__ dw) {
-  for (int r = blockIdx.x; r < v; r += gridDim.x) {
-  const int64_t slot = (int64_t)(r & ((1 << nb_log2) - 1)) * rows + (r >> nb_log2);
-  const int p0 = starts[slot], p1 = starts[slot + 1];
-  if (kAdd && p0 == p1) continue;
-  for (int col = threadIdx.x * 8; col < d; col += 2048) {
-    float sum[8] = {};
-    for (int p = p0; p < p1; ++p) {
-      float x[8];
-      Row8<T>::load(dout + (int64_t)sorted[p].y * ldx + col, x);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) sum[k] += x[k];
+__global__ __launch_bounds__(256) void k_embed_grad(EmbedSorted s, int v, const T* __restrict__ dout, int64_t ldx, int d,
+                                                    int per, int64_t chunk_units, int slices, float scale,
+                                                    TW* __restrict__ dw, float* __restrict__ parts) {
+  constexpr int kAhead = 8;
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  if (unit >= chunk_units) {
+    if (kAdd) return;
+    const int64_t r0 = (unit - chunk_units) * kFillRows;
+    bool empty = false;
+    if (lane < kFillRows && r0 + lane < v) {
+      const int64_t q = s.slot((int)(r0 + lane));
+      empty = s.starts[q] == s.starts[q + 1];
     }
-    TW* o = dw + (int64_t)r * d + col;
-    float old[8] = {};
-    if (kAdd) Row8<TW>::load(o, old);
+    const float zero[8] = {};
+    for (unsigned long long m = __ballot(empty); m; m &= m - 1) {
+      TW* o = dw + (r0 + __builtin_ctzll(m)) * d;
+      for (int col = lane * 8; col < d; col += 512) Row8<TW>::store(o + col, zero);
+    }
+    return;
+  }
+  const int chunk = (int)(unit / slices);
+  const int col = (int)(unit - (int64_t)chunk * slices) * kGradCols + lane * 8;
+  const bool live = col < d;
+  const int nv = s.count();
+  const int c0 = chunk * per, c1 = min(nv, c0 + per);
+  if (c0 >= c1) return;
+  const int before = c0 > 0 ? s.pairs[c0 - 1].x : -1, after = c1 < nv ? s.pairs[c1].x : -1;
+  float* part = parts + (int64_t)chunk * 2 * d + col;
+  float sum[8] = {};
+  int cur = s.pairs[c0].x;
+  bool first = true;               // still at the chunk's first id
+  const auto flush = [&](bool last) {
+    const bool from_before = first && cur == before, goes_on = last && cur == after;
+    first = false;
+    if (!live) return;
+    if (from_before || goes_on) Row8<float>::store(part + (from_before ? 0 : d), sum);
+    else grad_store<TW, kAdd>(dw + (int64_t)cur * d + col, sum, scale);
+  };
+  for (int g0 = c0; g0 < c1; g0 += 64) {
+    const int here = min(64, c1 - g0);
+    const int2 my = lane < here ? s.pairs[g0 + lane] : make_int2(-1, 0);
+    for (int p = 0; p < here; p += kAhead) {
+      float x[kAhead][8] = {};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum[k] = old[k] + scale * sum[k];
-    Row8<TW>::store(o, sum);
+      for (int k = 0; k < kAhead; ++k)
+        if (p + k < here && live) Row8<T>::load(dout + (int64_t)__builtin_amdgcn_readlane(my.y, p + k) * ldx + col, x[k]);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (p + k >= here) break;
+        const int r = __builtin_amdgcn_readlane(my.x, p + k);
+        if (r != cur) {
+          flush(false);
+          cur = r;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += x[k][e];
+      }
+    }
   }
+  flush(true);
+}
+
+// One workgroup per chunk and 512 columns; it has work where an id starts in the chunk and reaches past its end. Wave w
+// adds every fourth of the id's chunks from the w-th on; the waves' sums are added in order.
+template <typename TW, bool kAdd>
+__global__ __launch_bounds__(256) void k_embed_join(EmbedSorted s, int d, int per, int slices, float scale,
+                                                    TW* __restrict__ dw, const float* __restrict__ parts) {
+  __shared__ float sums[3][kGradCols];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int chunk = blockIdx.x / slices;
+  const int col = (blockIdx.x - chunk * slices) * kGradCols + lane * 8;
+  const int c0 = chunk * per, c1 = c0 + per;
+  if (c1 >= s.count()) return;
+  const int r = s.pairs[c1 - 1].x;
+  if (s.pairs[c1].x != r || (c0 > 0 && s.pairs[c0 - 1].x == r)) return;
+  const int last = (s.starts[s.slot(r) + 1] - 1) / per;        // the id's last chunk
+  const bool live = col < d;
+  float sum[8] = {};
+  if (live) {
+    if (w == 0) Row8<float>::load(parts + ((int64_t)chunk * 2 + 1) * d + col, sum);
+    for (int c = chunk + 1 + w; c <= last; c += 4) {
+      float x[8];
+      Row8<float>::load(parts + (int64_t)c * 2 * d + col, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += x[e];
+    }
+    if (w > 0)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sums[w - 1][e * 64 + lane] = sum[e];
   }
+  __syncthreads();
+  if (w > 0 || !live) return;
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += sums[k][e * 64 + lane];
+  grad_store<TW, kAdd>(dw + (int64_t)r * d + col, sum, scale);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -204,7 +343,9 @@ __global__ __launch_bounds__(256) void k_embed_grad(const int2* __restrict__ sor
 struct EmbedPlan {
   int64_t ldw, ldx, v_total;
   int nb_log2, rows;                 // buckets of the sort, ids of a bucket
-  size_t o_sorted, o_starts, bytes;
+  int per, slices;                   // tokens of a chunk, 512-column slices of a row
+  int64_t chunks;
+  size_t o_sorted, o_starts, o_parts, bytes;
 };
 
 inline bool known_dtype(int32_t t) { return t == LCE_DTYPE_BF16 || t == LCE_DTYPE_F32; }
@@ -233,6 +374,14 @@ lce_status_t make_embed_plan(const lce_embedding_t* p, EmbedPlan* pl) {
   size_t cur = 0;
   pl->o_sorted = take(cur, 8 * (size_t)p->n);
   pl->o_starts = take(cur, 4 * (((size_t)pl->rows << pl->nb_log2) + 1));
+  // tokens of a chunk: 8 to 64, for 4096 waves (16 per CU, each with eight rows' loads in flight); more where there
+  // would be more than 4096 chunks, whose two sums each bound the workspace
+  pl->slices = (int)((p->d + kGradCols - 1) / kGradCols);
+  pl->per = 8;
+  while (pl->per < 64 && p->n * pl->slices > (int64_t)4096 * pl->per) pl->per *= 2;
+  while (p->n > (int64_t)4096 * pl->per) pl->per *= 2;
+  pl->chunks = (p->n + pl->per - 1) / pl->per;
+  pl->o_parts = take(cur, 8 * (size_t)pl->chunks * p->d);
   pl->bytes = cur;
   return LCE_OK;
 }
@@ -245,12 +394,22 @@ void launch_lookup(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, c
     (const T*)W, pl.ldw, (int)p->d, p->scale, (T*)out, status);
 }
 
+template <typename T, typename TW, bool kAdd>
+void launch_embed_grad(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedSorted& s, const void* dout,
+                       void* dw, float* parts) {
+  const int64_t units = pl.chunks * pl.slices, fill = kAdd ? 0 : (p->v + kFillRows - 1) / kFillRows;
+  L(K_EMBED_GRAD, k_embed_grad<T, TW, kAdd>, dim3((unsigned)((units + fill + 3) / 4)), dim3(256), s, (int)p->v,
+    (const T*)dout, pl.ldx, (int)p->d, pl.per, units, pl.slices, p->scale, (TW*)dw, parts);
+  if (pl.chunks > 1)
+    L(K_EMBED_GRAD, k_embed_join<TW, kAdd>, dim3((unsigned)(pl.chunks * pl.slices)), dim3(256), s, (int)p->d, pl.per, pl.slices,
+      p->scale, (TW*)dw, (const float*)parts);
+}
+
 template <typename T, typename TW>
-void launch_embed_grad(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const int2* sorted, const int* starts,
-                       const void* dout, void* dw) {
-  const auto kernel = p->flags & LCE_FLAG_ACCUMULATE_DW ? k_embed_grad<T, TW, true> : k_embed_grad<T, TW, false>;
-  L(K_EMBED_GRAD, kernel, dim3((unsigned)std::min<int64_t>(p->v, 1 << 20)), dim3(256), sorted, starts, pl.nb_log2, pl.rows, (int)p->v, (const T*)dout, pl.ldx,
-    (int)p->d, p->scale, (TW*)dw);
+void launch_embed_grad(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedSorted& s, const void* dout,
+                       void* dw, float* parts) {
+  if (p->flags & LCE_FLAG_ACCUMULATE_DW) launch_embed_grad<T, TW, true>(L, p, pl, s, dout, dw, parts);
+  else launch_embed_grad<T, TW, false>(L, p, pl, s, dout, dw, parts);
 }
 
 }  // namespace
@@ -293,11 +452,15 @@ lce_status_t lce_embedding_backward(const lce_embedding_t* p, const void* ids, c
   char* ws = (char*)workspace;
   int2* sorted = (int2*)(ws + pl.o_sorted);
   int* starts = (int*)(ws + pl.o_starts);
-  const EmbedIds e{ids, p->id_bytes, p->n, p->v_begin, p->v, p->padding_idx};
-  L(K_EMBED_SORT, k_embed_sort, dim3(1u << pl.nb_log2), dim3(64 * kSortWaves), e, pl.nb_log2, pl.rows, sorted, starts);
-  if (p->dtype == LCE_DTYPE_F32) launch_embed_grad<float, float>(L, p, pl, sorted, starts, dOut, dW);
-  else if (p->dw_dtype == LCE_DTYPE_F32) launch_embed_grad<uint16_t, float>(L, p, pl, sorted, starts, dOut, dW);
-  else launch_embed_grad<uint16_t, uint16_t>(L, p, pl, sorted, starts, dOut, dW);
+  const bool pad = p->padding_idx >= p->v_begin && p->padding_idx < p->v_begin + p->v;
+  const EmbedRows e{ids, p->n, p->v_begin, (uint32_t)p->v, pad ? (int)(p->padding_idx - p->v_begin) : -1};
+  L(K_EMBED_SORT, p->id_bytes == 8 ? k_embed_sort<8> : k_embed_sort<4>, dim3(1u << pl.nb_log2), dim3(64 * kSortWaves), e,
+    pl.nb_log2, pl.rows, sorted, starts);
+  const EmbedSorted s{sorted, starts, pl.nb_log2, pl.rows};
+  float* parts = (float*)(ws + pl.o_parts);
+  if (p->dtype == LCE_DTYPE_F32) launch_embed_grad<float, float>(L, p, pl, s, dOut, dW, parts);
+  else if (p->dw_dtype == LCE_DTYPE_F32) launch_embed_grad<uint16_t, float>(L, p, pl, s, dOut, dW, parts);
+  else launch_embed_grad<uint16_t, uint16_t>(L, p, pl, s, dOut, dW, parts);
   return L.st;
 }
 
