@@ -13,12 +13,14 @@ namespace {
 // close together in a vocabulary ordered by frequency, fall into different buckets. One workgroup of 16 waves
 // serves a bucket on its own: it reads all N ids, counts those of lower buckets (which is where its bucket
 // starts) and, per wave and id, those of its own; a scan over (id, wave) gives every wave the place of its first
-// token of every id, and a second walk stores the token numbers. A wave owns consecutive tokens, so the order
-// within an id is the tokens'. No workgroup waits for another, and counts do not depend on an order.
+// token of every id, at which it then puts its tokens. A wave owns consecutive tokens, so the order within an id is
+// the tokens'. No workgroup waits for another, and counts do not depend on an order. A wave lists its tokens of the
+// bucket in LDS as it counts them, so only one with more than the list holds walks the ids twice.
 // ---------------------------------------------------------------------------------------------
 constexpr int kSortWaves = 16;
-constexpr int kSortIds = 512;      // most ids of a bucket
-constexpr int kSortAhead = 8;      // groups of 64 tokens whose ids a wave loads ahead
+constexpr int kSortIds = 1024;     // most ids of a bucket, one per thread in the scan
+constexpr int kSortAhead = 8;      // groups of 64 tokens whose ids a wave loads at a time
+constexpr int kSortList = 640;     // listed tokens of a wave; a round of loads adds up to 512
 
 // rows of W that get a gradient: id - v_begin in [0, v), other than the padding id's (pad_row, or -1)
 struct EmbedRows {
@@ -28,118 +30,128 @@ struct EmbedRows {
   int pad_row;
 };
 
-// the row of token i's id and its bucket, INT_MAX where the token has none
+// Of the wave's groups from token i on: the rows of the tokens' ids, and their buckets (INT_MAX where a token has
+// none). All loads are issued before the first is used: behind i1 they read the last token again.
 template <int kBytes>
-__device__ __forceinline__ int embed_bucket(const EmbedRows& e, int64_t i, int64_t i1, int mask, int* row) {
-  bool ok = i < i1;
-  uint32_t r = 0;
-  if (kBytes == 8) {
-    const uint64_t u = ok ? (uint64_t)(((const int64_t*)e.ids)[i] - e.v_begin) : 0;
-    ok &= u < e.v;
-    r = (uint32_t)u;
-  } else {
-    r = ok ? ((const uint32_t*)e.ids)[i] - (uint32_t)e.v_begin : 0;   // (v_begin + v <= 2^30: no id wraps into the rows)
-    ok &= r < e.v;
+__device__ __forceinline__ void embed_buckets(const EmbedRows& e, int64_t i, int64_t i1, int mask, int row[kSortAhead],
+                                              int bucket[kSortAhead]) {
+  typedef typename std::conditional<kBytes == 8, uint64_t, uint32_t>::type Id;
+  Id id[kSortAhead];
+#pragma unroll
+  for (int k = 0; k < kSortAhead; ++k) id[k] = ((const Id*)e.ids)[min(i + 64 * k, i1 - 1)];
+#pragma unroll
+  for (int k = 0; k < kSortAhead; ++k) {
+    const Id r = id[k] - (Id)e.v_begin;       // unsigned (v_begin + v <= 2^30: no other id wraps into the rows)
+    row[k] = (int)r;
+    bucket[k] = i + 64 * k < i1 && r < e.v && (int)r != e.pad_row ? (int)r & mask : 0x7FFFFFFF;
   }
-  *row = (int)r;
-  return ok && (int)r != e.pad_row ? (int)(r & mask) : 0x7FFFFFFF;
+}
+
+// What lanes of a wave wrote to LDS before is what its lanes read behind (the wave's LDS accesses are in order; the
+// compiler is told not to move them).
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The listed tokens of a wave, in order, to their places; place[q] is where the wave's next token of the bucket's
+// id q goes. 64 tokens at a time: a lane's rank among those with its id comes from one ballot per bit of the id.
+__device__ __forceinline__ void embed_place(const int2* list, int count, int* place_, int nb_log2, int rows, int lane,
+                                            int2* __restrict__ sorted) {
+  volatile int* place = place_;
+  for (int l = 0; l < count; l += 64) {
+    const bool in = l + lane < count;
+    const int2 pair = list[in ? l + lane : l];
+    const int q = pair.x >> nb_log2;
+    unsigned long long same = __ballot(in);
+    for (int bit = 0; (rows - 1) >> bit; ++bit) {
+      const unsigned long long m = __ballot((q >> bit) & 1);
+      same &= (q >> bit) & 1 ? m : ~m;
+    }
+    const int rank = __popcll(same & ((1ull << lane) - 1ull));
+    const int p = place[q] + rank;
+    if (in && rank == 0) place[q] = p + __popcll(same);
+    if (in) sorted[p] = pair;
+  }
 }
 
 template <int kBytes>
 __global__ __launch_bounds__(1024) void k_embed_sort(EmbedRows e, int nb_log2, int rows, int2* __restrict__ sorted,
                                                      int* __restrict__ starts) {
-  __shared__ int cnt[kSortIds * kSortWaves];   // [id of the bucket][wave]: count, then place of the next token
+  __shared__ int cnt[kSortWaves][kSortIds];    // per wave and id of the bucket: count, then place of the next token
+  __shared__ int2 lists[kSortWaves][kSortList];
   __shared__ int wsum[kSortWaves], below_all[kSortWaves];
   const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int mask = (1 << nb_log2) - 1, b = blockIdx.x;
-  for (int i = t; i < rows * kSortWaves; i += 1024) cnt[i] = 0;
-  __syncthreads();
+  for (int q = lane; q < rows; q += 64) cnt[w][q] = 0;      // its own entries only, until the scan
+  wave_lds_order();
   const int64_t per = (e.n + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
   const int64_t i0 = w * per, i1 = min(e.n, i0 + per);
-  int below = 0;
-  unsigned long long hits = 0;       // bit g: the wave's groups g, g + 64, ... hold tokens of the bucket
-  int g = 0;
-  for (int64_t i = i0; i < i1; i += 64 * kSortAhead, g += kSortAhead) {
-    int r[kSortAhead], rb[kSortAhead];
-#pragma unroll
-    for (int k = 0; k < kSortAhead; ++k) rb[k] = embed_bucket<kBytes>(e, i + 64 * k + lane, i1, mask, &r[k]);
+  int2* list = lists[w];
+  int r[kSortAhead], rb[kSortAhead], below = 0, mine = 0;
+  for (int64_t i = i0; i < i1; i += 64 * kSortAhead) {
+    embed_buckets<kBytes>(e, i + lane, i1, mask, r, rb);
 #pragma unroll
     for (int k = 0; k < kSortAhead; ++k) {
       below += rb[k] < b;
-      if (rb[k] == b) atomicAdd(&cnt[(r[k] >> nb_log2) * kSortWaves + w], 1);
-      hits |= (unsigned long long)(__ballot(rb[k] == b) != 0) << ((g + k) & 63);
+      const unsigned long long m = __ballot(rb[k] == b);
+      if (m == 0) continue;
+      if (rb[k] == b) {
+        atomicAdd(&cnt[w][r[k] >> nb_log2], 1);
+        const int l = mine + __popcll(m & ((1ull << lane) - 1ull));
+        if (l < kSortList) list[l] = make_int2(r[k], (int)(i + 64 * k + lane));
+      }
+      mine += __popcll(m);
     }
   }
   for (int m = 32; m >= 1; m >>= 1) below += __shfl_xor(below, m);
   if (lane == 0) below_all[w] = below;
   __syncthreads();
-  int base = 0;
-  for (int k = 0; k < kSortWaves; ++k) base += below_all[k];
-  // exclusive scan of cnt: 8 consecutive entries per thread
-  constexpr int kPer = kSortIds * kSortWaves / 1024;
-  int own[kPer], sum = 0;
+  // thread t: the tokens of the bucket's id t, wave by wave, and of all ids before
+  int own[kSortWaves], sum = 0;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int j = t * kPer + k;
-    own[k] = j < rows * kSortWaves ? cnt[j] : 0;
+  for (int k = 0; k < kSortWaves; ++k) {
+    own[k] = t < rows ? cnt[k][t] : 0;
     sum += own[k];
   }
-  int incl = sum;
+  int at = sum;
   for (int m = 1; m < 64; m <<= 1) {
-    const int o = __shfl_up(incl, m);
-    if (lane >= m) incl += o;
+    const int o = __shfl_up(at, m);
+    if (lane >= m) at += o;
   }
-  if (lane == 63) wsum[w] = incl;
+  if (lane == 63) wsum[w] = at;
   __syncthreads();
-  int at = base + incl - sum;
-  for (int k = 0; k < w; ++k) at += wsum[k];
+  at -= sum;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int j = t * kPer + k;
-    if (j < rows * kSortWaves) {
-      cnt[j] = at;
-      if (j % kSortWaves == 0) starts[(int64_t)b * rows + j / kSortWaves] = at;
+  for (int k = 0; k < kSortWaves; ++k) at += below_all[k] + (k < w ? wsum[k] : 0);
+  if (t < rows) {
+    starts[(int64_t)b * rows + t] = at;
+    if (b == mask && t == rows - 1) starts[(int64_t)b * rows + rows] = at + sum;
+#pragma unroll
+    for (int k = 0; k < kSortWaves; ++k) {
+      cnt[k][t] = at;
+      at += own[k];
     }
-    at += own[k];
   }
-  if (b == mask && t == 1023) starts[((int64_t)mask + 1) * rows] = at;
   __syncthreads();
-  g = 0;
-  for (int64_t i = i0; i < i1; i += 64 * kSortAhead, g += kSortAhead) {
-    if (((hits >> (g & 63)) & ((1u << kSortAhead) - 1)) == 0) continue;
-    int r[kSortAhead], rb[kSortAhead];
-#pragma unroll
-    for (int k = 0; k < kSortAhead; ++k) rb[k] = embed_bucket<kBytes>(e, i + 64 * k + lane, i1, mask, &r[k]);
+  if (mine <= kSortList) {
+    embed_place(list, mine, cnt[w], nb_log2, rows, lane, sorted);
+    return;
+  }
+  mine = 0;
+  for (int64_t i = i0; i < i1; i += 64 * kSortAhead) {
+    embed_buckets<kBytes>(e, i + lane, i1, mask, r, rb);
 #pragma unroll
     for (int k = 0; k < kSortAhead; ++k) {
-      unsigned long long todo = __ballot(rb[k] == b);
-      if (todo == 0) continue;
-      const int q = r[k] >> nb_log2;
-      const int2 pair = make_int2(r[k], (int)(i + 64 * k + lane));
-      // the lanes of one id after the other, for the first few ids (a group has 64 / nb of a bucket's tokens on
-      // average, besides a frequent id's) ...
-      for (int few = 0; todo && few < 3; ++few) {
-        const int q1 = __builtin_amdgcn_readlane(q, __builtin_ctzll(todo));
-        const unsigned long long same = __ballot(rb[k] == b && q == q1);
-        volatile int* place = &cnt[q1 * kSortWaves + w];   // this wave's own entries
-        const int p = *place;
-        if (rb[k] == b && q == q1) sorted[p + __popcll(same & ((1ull << lane) - 1ull))] = pair;
-        if (lane == 0) *place = p + __popcll(same);
-        todo &= ~same;
-      }
-      if (todo == 0) continue;
-      // ... and all others at once: the lanes with this lane's id, from one ballot per bit of it
-      const bool in = (todo >> lane) & 1;
-      unsigned long long same = todo;
-      for (int bit = 0; (rows - 1) >> bit; ++bit) {
-        const unsigned long long m = __ballot((q >> bit) & 1);
-        same &= (q >> bit) & 1 ? m : ~m;
-      }
-      volatile int* place = &cnt[(in ? q : 0) * kSortWaves + w];
-      const int rank = __popcll(same & ((1ull << lane) - 1ull));
-      const int p = *place + rank;
-      if (in && rank == 0) *place = p + __popcll(same);
-      if (in) sorted[p] = pair;
+      const unsigned long long m = __ballot(rb[k] == b);
+      if (rb[k] == b) list[mine + __popcll(m & ((1ull << lane) - 1ull))] = make_int2(r[k], (int)(i + 64 * k + lane));
+      mine += __popcll(m);
+    }
+    if (mine > kSortList - 64 * kSortAhead || i + 64 * kSortAhead >= i1) {
+      wave_lds_order();
+      embed_place(list, mine, cnt[w], nb_log2, rows, lane, sorted);
+      wave_lds_order();
+      mine = 0;
     }
   }
 }
@@ -318,11 +330,15 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedSorted s, int d, int pe
   float sum[8] = {};
   if (live) {
     if (w == 0) Row8<float>::load(parts + ((int64_t)chunk * 2 + 1) * d + col, sum);
-    for (int c = chunk + 1 + w; c <= last; c += 4) {
-      float x[8];
-      Row8<float>::load(parts + (int64_t)c * 2 * d + col, x);
+    for (int c = chunk + 1 + w; c <= last; c += 16) {
+      float x[4][8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += x[e];
+      for (int k = 0; k < 4; ++k) Row8<float>::load(parts + (int64_t)min(c + 4 * k, last) * 2 * d + col, x[k]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + 4 * k <= last)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum[e] += x[k][e];
     }
     if (w > 0)
 #pragma unroll
