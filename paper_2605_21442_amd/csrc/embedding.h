@@ -224,10 +224,8 @@ __global__ void k_embed_clear_status(int* status) { *status = 0; }
 // that reaches over a chunk's edge leaves an fp32 sum per chunk, in the chunk's slot 0 where it goes on from the chunk
 // before and in slot 1 where it starts, and k_embed_join adds these in the order of the chunks. So a frequent id
 // is spread over many waves, and the order of all sums follows from the ids and N alone.
-// Behind the chunks the same launch zeroes the rows of a fresh dW that have no token.
 // ---------------------------------------------------------------------------------------------
 constexpr int kGradCols = 512;     // columns of a wave
-constexpr int kFillRows = 16;      // ids whose rows a wave zeroes, where they have no token
 
 struct EmbedSorted {
   const int2* pairs;               // (row of W, token), by id
@@ -247,27 +245,13 @@ __device__ __forceinline__ void grad_store(TW* o, const float sum[8], float scal
 }
 
 template <typename T, typename TW, bool kAdd>
-__global__ __launch_bounds__(256) void k_embed_grad(EmbedSorted s, int v, const T* __restrict__ dout, int64_t ldx, int d,
+__global__ __launch_bounds__(256) void k_embed_grad(EmbedSorted s, const T* __restrict__ dout, int64_t ldx, int d,
                                                     int per, int64_t chunk_units, int slices, float scale,
                                                     TW* __restrict__ dw, float* __restrict__ parts) {
   constexpr int kAhead = 8;
   const int lane = threadIdx.x & 63;
-  const int64_t unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
-  if (unit >= chunk_units) {
-    if (kAdd) return;
-    const int64_t r0 = (unit - chunk_units) * kFillRows;
-    bool empty = false;
-    if (lane < kFillRows && r0 + lane < v) {
-      const int64_t q = s.slot((int)(r0 + lane));
-      empty = s.starts[q] == s.starts[q + 1];
-    }
-    const float zero[8] = {};
-    for (unsigned long long m = __ballot(empty); m; m &= m - 1) {
-      TW* o = dw + (r0 + __builtin_ctzll(m)) * d;
-      for (int col = lane * 8; col < d; col += 512) Row8<TW>::store(o + col, zero);
-    }
-    return;
-  }
+  const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  if (unit >= chunk_units) return;
   const int chunk = (int)(unit / slices);
   const int col = (int)(unit - (int64_t)chunk * slices) * kGradCols + lane * 8;
   const bool live = col < d;
@@ -312,12 +296,42 @@ __global__ __launch_bounds__(256) void k_embed_grad(EmbedSorted s, int v, const 
   flush(true);
 }
 
-// One workgroup per chunk and 512 columns; it has work where an id starts in the chunk and reaches past its end. Wave w
-// adds every fourth of the id's chunks from the w-th on; the waves' sums are added in order.
+// The rows of a fresh dW without a token, in the order of the addresses: 16 KB of dW per workgroup, 16 bytes of each
+// 4 KB per thread. (128256 x 4096 bf16 in pieces of 16 KB: 6.7 TB/s, as a fill without a look at the rows; of 4 KB, whose
+// two loads come before the one store, 5.1; whole rows by wave 5.5 to 6.0.)
+constexpr int kFillAhead = 4;
+constexpr int64_t kFillBytes = 256 * 16 * kFillAhead;
+
+template <typename TW>
+__device__ __forceinline__ void embed_fill(const EmbedSorted& s, int64_t block, int v, int d, TW* __restrict__ dw) {
+  const uint32_t row16 = (uint32_t)(d * sizeof(TW) / 16);
+  const int64_t r0 = block * (kFillBytes / 16) / row16;
+  const uint32_t o0 = (uint32_t)(block * (kFillBytes / 16) - r0 * row16);
+  bool empty[kFillAhead];
+#pragma unroll
+  for (int k = 0; k < kFillAhead; ++k) {
+    const int64_t at = r0 + (o0 + threadIdx.x + 256 * k) / row16;
+    const int64_t q = s.slot((int)min(at, (int64_t)v - 1));
+    empty[k] = at < v && s.starts[q] == s.starts[q + 1];
+  }
+  char* o = reinterpret_cast<char*>(dw) + block * kFillBytes + 16 * threadIdx.x;
+#pragma unroll
+  for (int k = 0; k < kFillAhead; ++k)
+    if (empty[k]) store16_padded(o + 4096 * k, i32x4_t{0, 0, 0, 0});
+}
+
+// The sums of ids that several chunks share: one workgroup per chunk and 512 columns, which has work where an id starts in
+// the chunk and reaches past its end. Wave w adds every fourth of the id's chunks from the w-th on, four loads in flight; the
+// waves' sums are added in order. Behind these workgroups come those of embed_fill: here they have the 32 waves a
+// CU holds, which the registers of k_embed_grad would halve (709 tokens, 128256 x 2048: 100 us there).
 template <typename TW, bool kAdd>
-__global__ __launch_bounds__(256) void k_embed_join(EmbedSorted s, int d, int per, int slices, float scale,
-                                                    TW* __restrict__ dw, const float* __restrict__ parts) {
+__global__ __launch_bounds__(256) void k_embed_join(EmbedSorted s, int v, int d, int per, int slices, int64_t join_blocks,
+                                                    float scale, TW* __restrict__ dw, const float* __restrict__ parts) {
   __shared__ float sums[3][kGradCols];
+  if (!kAdd && blockIdx.x >= join_blocks) {
+    embed_fill<TW>(s, blockIdx.x - join_blocks, v, d, dw);
+    return;
+  }
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int chunk = blockIdx.x / slices;
   const int col = (blockIdx.x - chunk * slices) * kGradCols + lane * 8;
@@ -413,12 +427,12 @@ void launch_lookup(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, c
 template <typename T, typename TW, bool kAdd>
 void launch_embed_grad(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedSorted& s, const void* dout,
                        void* dw, float* parts) {
-  const int64_t units = pl.chunks * pl.slices, fill = kAdd ? 0 : (p->v + kFillRows - 1) / kFillRows;
-  L(K_EMBED_GRAD, k_embed_grad<T, TW, kAdd>, dim3((unsigned)((units + fill + 3) / 4)), dim3(256), s, (int)p->v,
-    (const T*)dout, pl.ldx, (int)p->d, pl.per, units, pl.slices, p->scale, (TW*)dw, parts);
-  if (pl.chunks > 1)
-    L(K_EMBED_GRAD, k_embed_join<TW, kAdd>, dim3((unsigned)(pl.chunks * pl.slices)), dim3(256), s, (int)p->d, pl.per, pl.slices,
-      p->scale, (TW*)dw, (const float*)parts);
+  const int64_t units = pl.chunks * pl.slices, join = pl.chunks > 1 ? units : 0;
+  const int64_t fill = kAdd ? 0 : (p->v * p->d * (int64_t)sizeof(TW) + kFillBytes - 1) / kFillBytes;
+  L(K_EMBED_GRAD, k_embed_grad<T, TW, kAdd>, dim3((unsigned)((units + 3) / 4)), dim3(256), s, (const T*)dout, pl.ldx,
+    (int)p->d, pl.per, units, pl.slices, p->scale, (TW*)dw, parts);
+  L(K_EMBED_GRAD, k_embed_join<TW, kAdd>, dim3((unsigned)(join + fill)), dim3(256), s, (int)p->v, (int)p->d, pl.per,
+    pl.slices, join, p->scale, (TW*)dw, (const float*)parts);
 }
 
 template <typename T, typename TW>
