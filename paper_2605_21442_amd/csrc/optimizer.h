@@ -19,7 +19,8 @@ struct AdamWEntry {
   int64_t n;
   uint32_t first;          // first workgroup of this tensor
   uint32_t pair0;          // place / 2
-  uint8_t group, param_f32, grad_f32, pad_[5];
+  uint8_t group, param_f32, grad_f32;
+  uint8_t wide;            // bits: param, grad, master lie at a multiple of 16 bytes
 };
 
 struct AdamWTable {
@@ -29,36 +30,88 @@ struct AdamWTable {
 };
 static_assert(sizeof(AdamWTable) <= 4000, "launch arguments");
 
+// The entry of workgroup `block`: the last one whose first workgroup is not behind it, found by all lanes at once.
+template <typename Entry>
+__device__ __forceinline__ int table_entry(const Entry* e, int count, uint32_t block) {
+  int k = -1;
+  for (int i = 0; i < count; i += 64) {
+    const int j = i + (threadIdx.x & 63);
+    k += __popcll(__ballot(j < count && e[min(j, count - 1)].first <= block));
+  }
+  return __builtin_amdgcn_readfirstlane(k);
+}
+
+// N consecutive elements from i on as fp32, and back; elements at or past n are 0 and are not touched. `wide`: the
+// tensor's address is a multiple of 16 bytes (i is a multiple of N).
+template <int N>
+__device__ __forceinline__ void load_elems(const void* p, int64_t i, int64_t n, bool f32, bool wide, float x[N]) {
+  if (wide && i + N <= n) {
+    if (f32) {
+#pragma unroll
+      for (int h = 0; h < N / 4; ++h) {
+        const float4 a = *reinterpret_cast<const float4*>((const float*)p + i + 4 * h);
+        x[4 * h] = a.x; x[4 * h + 1] = a.y; x[4 * h + 2] = a.z; x[4 * h + 3] = a.w;
+      }
+    } else {
+      typedef uint32_t Words __attribute__((ext_vector_type(N / 2)));
+      const Words a = *reinterpret_cast<const Words*>((const uint16_t*)p + i);
+#pragma unroll
+      for (int h = 0; h < N / 2; ++h) { x[2 * h] = __uint_as_float(a[h] << 16); x[2 * h + 1] = __uint_as_float(a[h] & 0xFFFF0000u); }
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    x[k] = i + k >= n ? 0.f : f32 ? ((const float*)p)[i + k] : bf16_to_f32(((const uint16_t*)p)[i + k]);
+}
+
+template <int N>
+__device__ __forceinline__ void store_elems(void* p, int64_t i, int64_t n, bool f32, bool wide, const float x[N]) {
+  if (wide && i + N <= n) {
+    if (f32) {
+#pragma unroll
+      for (int h = 0; h < N / 4; ++h)
+        store16_padded((float*)p + i + 4 * h, i32x4_t{(int)__float_as_uint(x[4 * h]), (int)__float_as_uint(x[4 * h + 1]),
+                                                      (int)__float_as_uint(x[4 * h + 2]), (int)__float_as_uint(x[4 * h + 3])});
+    } else if (N == 8) {
+      store16_padded((uint16_t*)p + i, i32x4_t{(int)pack_bf16x2(x[0], x[1]), (int)pack_bf16x2(x[2], x[3]),
+                                               (int)pack_bf16x2(x[N - 4], x[N - 3]), (int)pack_bf16x2(x[N - 2], x[N - 1])});
+    } else {
+      *reinterpret_cast<u32x2_t*>((uint16_t*)p + i) = u32x2_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    if (i + k >= n) break;
+    if (f32) ((float*)p)[i + k] = x[k];
+    else ((uint16_t*)p)[i + k] = to_bf16(x[k]);
+  }
+}
+
 // ---------------------------------------------------------------------------------------------
 // 8-bit moments (the form is in lce.h). kMant 3: sign and 7 bits; kMant 4: 8 bits, no sign.
+//
+// A code shifted to the top of an fp32 mantissa, its upper 4 bits in the exponent field, is an fp32 number: the
+// code's q times 2^-(126 + kMant), subnormal where the code is below 2^kMant. So decoding is a shift and an exact
+// scaling, and rounding stochastically is adding random bits below the code and cutting them off.
 // ---------------------------------------------------------------------------------------------
-__device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
-
 // unit byte of a block from the bits of its largest magnitude (as an unsigned number, which orders
 // magnitudes, and infinities and NaN above them)
 template <int kMant>
 __device__ __forceinline__ int unit_byte(uint32_t top) {
-  if (top >= 0x7F800000u) return 255;
   const int s = (int)((top + (1u << (23 - kMant))) >> 23) - 14 - kMant;
-  return s < 1 ? 1 : s;
+  return top >= 0x7F800000u ? 255 : s < 1 ? 1 : s;
 }
 
-// code of magnitude a >= 0 in units of 2^(s - 127); u in [0, 1): upward from the code below where the place
-// between the two is at least 1 - u
+// exponent that takes a code's fp32 number to its value in units of 2^(s - 127)
 template <int kMant>
-__device__ __forceinline__ uint32_t encode(float a, int s, float u) {
-#pragma clang fp contract(off)
-  const float y = a * pow2f(127 - s);              // exact
-  int h = (int)(__float_as_uint(y) >> 23) - 127 - kMant;
-  h = h < 0 ? 0 : h;
-  return (uint32_t)floorf(y * pow2f(-h) + u) + ((uint32_t)h << kMant);
-}
+__device__ __forceinline__ int code_exponent(int s) { return s - 1 + kMant; }
 
+// code (kMant 3: with the sign in bit 11) of x; bits: 16 random bits
 template <int kMant>
-__device__ __forceinline__ float decode(uint32_t c, int s) {
-  const int h = (int)(c >> kMant);
-  const float q = (float)(h ? (c & ((1u << kMant) - 1)) + (1u << kMant) : c);
-  return q * (s == 255 ? __uint_as_float(0x7FC00000u) : pow2f((h ? h - 1 : 0) + s - 127));
+__device__ __forceinline__ uint32_t encode(float x, int s, uint32_t bits) {
+  return (__float_as_uint(ldexpf(x, -code_exponent<kMant>(s))) + (bits << (7 - kMant))) >> (23 - kMant);
 }
 
 // 16 random bits for each of two neighbouring elements: a multiplicative hash (Knuth, TAOCP 6.4) of the
@@ -71,85 +124,164 @@ __device__ __forceinline__ uint32_t pair_bits(uint32_t pair, uint32_t seed) {
   return x ^ (x >> 16);
 }
 
-__device__ __forceinline__ float load_elem(const void* p, int64_t i, bool f32) {
-  return f32 ? ((const float*)p)[i] : bf16_to_f32(((const uint16_t*)p)[i]);
+// the largest of four neighbouring lanes
+__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true));   // lanes 1 0 3 2
+  return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));   // lanes 2 3 0 1
 }
 
-constexpr int kStepElems = 4096;       // elements of a workgroup
+// 8 elements' moments from their bytes
+__device__ __forceinline__ void decode_moments(const uint2 cm, const uint2 cr, int sm, int sr, float m[8], float r[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t wm = k < 4 ? cm.x : cm.y, wr = k < 4 ? cr.x : cr.y;
+    const int c = (int)(wm << (24 - 8 * (k & 3))) >> 4;           // sign, copies of it, 7-bit code
+    m[k] = ldexpf(__uint_as_float((uint32_t)c & 0x87F00000u), code_exponent<3>(sm));
+    r[k] = ldexpf(__uint_as_float((wr >> (8 * (k & 3)) & 255u) << 19), code_exponent<4>(sr));
+  }
+  const float nan = __uint_as_float(0x7FC00000u);
+  if (sm == 255)
+    for (int k = 0; k < 8; ++k) m[k] = nan;
+  if (sr == 255)
+    for (int k = 0; k < 8; ++k) r[k] = nan;
+}
 
-// One element per thread and step; the 32 lanes of a half wave are a block of the 8-bit moments.
+constexpr int kStepElems = 8192;       // elements of a workgroup
+static_assert(kStepElems % 2048 == 0, "whole rounds of either form");
+
+// 32-bit moments: 4 elements per thread and round, so that every access of a wave is contiguous.
+__device__ __forceinline__ void adamw_round32(const AdamWEntry& e, const AdamWConst& c, int64_t i, float scale, bool scaled) {
+#pragma clang fp contract(off)
+  float p[4], g[4] = {}, m[4], v[4];
+  load_elems<4>(e.m, i, e.n, true, true, m);
+  load_elems<4>(e.v, i, e.n, true, true, v);
+  if (e.master) load_elems<4>(e.master, i, e.n, true, e.wide & 4, p);
+  else load_elems<4>(e.param, i, e.n, e.param_f32, e.wide & 1, p);
+  if (e.grad) load_elems<4>(e.grad, i, e.n, e.grad_f32, e.wide & 2, g);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (scaled) g[k] = g[k] * scale;
+    adamw_update(p[k], m[k], v[k], g[k], c);
+  }
+  store_elems<4>(e.m, i, e.n, true, true, m);
+  store_elems<4>(e.v, i, e.n, true, true, v);
+  if (e.master) store_elems<4>(e.master, i, e.n, true, e.wide & 4, p);
+  store_elems<4>(e.param, i, e.n, e.param_f32, e.wide & 1, p);
+}
+
+// 8-bit moments: 8 elements per thread and round, four lanes to a block. Every lane of a wave comes here (the
+// blocks' maxima pass between lanes); those at or past n hold zeros.
+__device__ __forceinline__ void adamw_round8(const AdamWEntry& e, const AdamWConst& c, int64_t i, float scale, bool scaled,
+                                             uint32_t seed) {
+#pragma clang fp contract(off)
+  float p[8] = {}, g[8] = {}, m[8] = {}, r[8] = {};
+  uint8_t* units = e.units + 2 * (i / kMomentBlock);
+  uint2 cm = make_uint2(0, 0), cr = cm;
+  int s = 0;
+  const bool whole = i + 8 <= e.n;
+  if (i < e.n) {
+    s = *reinterpret_cast<const uint16_t*>(units);
+    if (whole) {
+      cm = *reinterpret_cast<const uint2*>((const uint8_t*)e.m + i);
+      cr = *reinterpret_cast<const uint2*>((const uint8_t*)e.v + i);
+    } else {
+      for (int k = 0; k < (int)(e.n - i); ++k) {
+        const uint32_t a = ((const uint8_t*)e.m)[i + k], b = ((const uint8_t*)e.v)[i + k];
+        if (k < 4) { cm.x |= a << 8 * k; cr.x |= b << 8 * k; }
+        else { cm.y |= a << 8 * (k - 4); cr.y |= b << 8 * (k - 4); }
+      }
+    }
+    if (e.master) load_elems<8>(e.master, i, e.n, true, e.wide & 4, p);
+    else load_elems<8>(e.param, i, e.n, e.param_f32, e.wide & 1, p);
+    if (e.grad) load_elems<8>(e.grad, i, e.n, e.grad_f32, e.wide & 2, g);
+    decode_moments(cm, cr, s & 255, s >> 8, m, r);
+  }
+  uint32_t am = 0, ar = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if (scaled) g[k] = g[k] * scale;
+    float v = r[k] * r[k];
+    r[k] = adamw_update_root(p[k], m[k], v, g[k], c);
+    if (whole || i + k < e.n) {
+      am = max(am, __float_as_uint(m[k]) & 0x7FFFFFFFu);
+      ar = max(ar, __float_as_uint(r[k]) & 0x7FFFFFFFu);
+    }
+  }
+  const int sm = unit_byte<3>(quad_max(am)), sr = unit_byte<4>(quad_max(ar));
+  if (i >= e.n) return;
+  uint32_t bm[8], br[8];
+#pragma unroll
+  for (int k = 0; k < 8; k += 2) {
+    const uint32_t h = pair_bits(e.pair0 + (uint32_t)(i >> 1) + k / 2, seed);
+#pragma unroll
+    for (int j = k; j < k + 2; ++j) {
+      const uint32_t bits = j & 1 ? h >> 16 : h & 0xFFFFu;
+      const uint32_t x = encode<3>(m[j], sm, bits);
+      bm[j] = (x & 0x7Fu) | (x >> 4 & 0x80u);
+      br[j] = max(encode<4>(r[j], sr, bits), r[j] > 0.f ? 1u : 0u);
+    }
+  }
+  if (sm == 255)
+    for (int k = 0; k < 8; ++k) bm[k] = 0;
+  if (sr == 255)
+    for (int k = 0; k < 8; ++k) br[k] = 0;
+  if (whole) {
+    *reinterpret_cast<uint2*>((uint8_t*)e.m + i) =
+        make_uint2(bm[0] | bm[1] << 8 | bm[2] << 16 | bm[3] << 24, bm[4] | bm[5] << 8 | bm[6] << 16 | bm[7] << 24);
+    *reinterpret_cast<uint2*>((uint8_t*)e.v + i) =
+        make_uint2(br[0] | br[1] << 8 | br[2] << 16 | br[3] << 24, br[4] | br[5] << 8 | br[6] << 16 | br[7] << 24);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (i + k >= e.n) break;
+      ((uint8_t*)e.m)[i + k] = (uint8_t)bm[k];
+      ((uint8_t*)e.v)[i + k] = (uint8_t)br[k];
+    }
+  }
+  if (i % kMomentBlock == 0) *reinterpret_cast<uint16_t*>(units) = (uint16_t)(sm | sr << 8);
+  if (e.master) store_elems<8>(e.master, i, e.n, true, e.wide & 4, p);
+  store_elems<8>(e.param, i, e.n, e.param_f32, e.wide & 1, p);
+}
+
 template <int kBits>
 __global__ __launch_bounds__(256) void k_adamw_tensors(AdamWTable t, const float* __restrict__ grad_scale, uint32_t seed) {
-#pragma clang fp contract(off)
   const float scale = grad_scale ? *grad_scale : 1.0f;
   if (!(fabsf(scale) < INFINITY)) return;
-  int k = 0;
-  while (k + 1 < t.count && t.e[k + 1].first <= blockIdx.x) ++k;
-  const AdamWEntry& e = t.e[k];
+  const AdamWEntry e = t.e[table_entry(t.e, t.count, blockIdx.x)];
   const AdamWConst c = t.g[e.group];
+  constexpr int kPer = kBits == 32 ? 4 : 8;
   const int64_t i0 = (int64_t)(blockIdx.x - e.first) * kStepElems;
-  for (int j = 0; j < kStepElems; j += 256) {
-    if (i0 + j >= e.n) break;                     // uniform
-    const int64_t i = i0 + j + threadIdx.x;
-    const bool live = i < e.n;
-    const int64_t blk = i / kMomentBlock;
-    float p = 0.f, g = 0.f, m = 0.f, v = 0.f;
-    if (live) {
-      p = e.master ? e.master[i] : load_elem(e.param, i, e.param_f32);
-      if (e.grad) g = load_elem(e.grad, i, e.grad_f32);
-      if (kBits == 32) {
-        m = ((float*)e.m)[i];
-        v = ((float*)e.v)[i];
-      } else {
-        const uint32_t cm = ((const uint8_t*)e.m)[i];
-        const float x = decode<3>(cm & 127, e.units[2 * blk]), r = decode<4>(((const uint8_t*)e.v)[i], e.units[2 * blk + 1]);
-        m = cm & 128 ? -x : x;
-        v = r * r;
-      }
-    }
-    if (grad_scale) g = g * scale;
-    adamw_update(p, m, v, g, c);
-    if (kBits == 8) {
-      const float root = sqrtf(v);
-      uint32_t am = live ? __float_as_uint(m) & 0x7FFFFFFFu : 0, ar = live ? __float_as_uint(root) & 0x7FFFFFFFu : 0;
-      for (int x = 16; x >= 1; x >>= 1) {
-        am = max(am, (uint32_t)__shfl_xor((int)am, x));
-        ar = max(ar, (uint32_t)__shfl_xor((int)ar, x));
-      }
-      const int sm = unit_byte<3>(am), sr = unit_byte<4>(ar);
-      if (live) {
-        const uint32_t h = pair_bits(e.pair0 + (uint32_t)(i >> 1), seed);
-        const float u = (float)(i & 1 ? h >> 16 : h & 0xFFFFu) * 0x1p-16f;
-        const uint32_t cm = sm == 255 ? 0 : encode<3>(fabsf(m), sm, u);
-        uint32_t cr = sr == 255 ? 0 : encode<4>(root, sr, u);
-        if (root > 0.f && cr == 0) cr = 1;
-        ((uint8_t*)e.m)[i] = (uint8_t)(cm | (__float_as_uint(m) >> 24 & 128));
-        ((uint8_t*)e.v)[i] = (uint8_t)cr;
-        if (i % kMomentBlock == 0) {
-          e.units[2 * blk] = (uint8_t)sm;
-          e.units[2 * blk + 1] = (uint8_t)sr;
-        }
-      }
-    } else if (live) {
-      ((float*)e.m)[i] = m;
-      ((float*)e.v)[i] = v;
-    }
-    if (live) {
-      if (e.master) e.master[i] = p;
-      if (e.param_f32) ((float*)e.param)[i] = p;
-      else ((uint16_t*)e.param)[i] = to_bf16(p);
+  for (int j = 0; j < kStepElems && i0 + j < e.n; j += 256 * kPer) {
+    const int64_t i = i0 + j + kPer * threadIdx.x;
+    if constexpr (kBits == 32) {
+      if (i < e.n) adamw_round32(e, c, i, scale, grad_scale != nullptr);
+    } else {
+      adamw_round8(e, c, i, scale, grad_scale != nullptr, seed);
     }
   }
 }
 
+// 8 elements per thread
 __global__ __launch_bounds__(256) void k_adamw_moments(int64_t n, const uint8_t* __restrict__ m, const uint8_t* __restrict__ r,
                                                        const uint8_t* __restrict__ units, uint16_t* __restrict__ first,
                                                        uint16_t* __restrict__ root) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (i >= n) return;
-  const float x = decode<3>(m[i] & 127, units[2 * (i / kMomentBlock)]);
-  first[i] = to_bf16(m[i] & 128 ? -x : x);
-  root[i] = to_bf16(decode<4>(r[i], units[2 * (i / kMomentBlock) + 1]));
+  const int s = *reinterpret_cast<const uint16_t*>(units + 2 * (i / kMomentBlock));
+  float x[8], y[8];
+  uint2 cm = make_uint2(0, 0), cr = cm;
+  if (i + 8 <= n) {
+    cm = *reinterpret_cast<const uint2*>(m + i);
+    cr = *reinterpret_cast<const uint2*>(r + i);
+  } else {
+    for (int k = 0; k < (int)(n - i); ++k) {
+      if (k < 4) { cm.x |= (uint32_t)m[i + k] << 8 * k; cr.x |= (uint32_t)r[i + k] << 8 * k; }
+      else { cm.y |= (uint32_t)m[i + k] << 8 * (k - 4); cr.y |= (uint32_t)r[i + k] << 8 * (k - 4); }
+    }
+  }
+  decode_moments(cm, cr, s & 255, s >> 8, x, y);
+  store_elems<8>(first, i, n, false, true, x);
+  store_elems<8>(root, i, n, false, true, y);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -168,7 +300,6 @@ struct NormTable {
   int count;
 };
 static_assert(sizeof(NormTable) <= 4000, "launch arguments");
-constexpr int kNormElems = 16384;      // elements of a workgroup
 
 __device__ __forceinline__ double block_sum_f64(double x) {
   __shared__ double part[4];
@@ -178,16 +309,48 @@ __device__ __forceinline__ double block_sum_f64(double x) {
   return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-__global__ __launch_bounds__(256) void k_grad_squares(NormTable t, double* __restrict__ parts) {
-  int k = 0;
-  while (k + 1 < t.count && t.e[k + 1].first <= blockIdx.x) ++k;
-  const NormEntry& e = t.e[k];
-  const int64_t i0 = (int64_t)(blockIdx.x - e.first) * kNormElems;
-  const int64_t i1 = min(e.n, i0 + kNormElems);
+__device__ __forceinline__ double squares(const uint4 a, bool f32) {
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+  double lo = 0, hi = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (f32) {
+      const double x = __uint_as_float(w[k]);
+      lo = fma(x, x, lo);
+    } else {
+      const double x = __uint_as_float(w[k] << 16), y = __uint_as_float(w[k] & 0xFFFF0000u);
+      lo = fma(x, x, lo);
+      hi = fma(y, y, hi);
+    }
+  }
+  return lo + hi;
+}
+
+// A workgroup takes `bytes` bytes of a tensor in 16-byte pieces, eight in flight per thread; the tensor's elements before the
+// first multiple of 16 bytes and behind the last are added one by one by its first workgroup.
+__global__ __launch_bounds__(256) void k_grad_squares(NormTable t, int64_t bytes, double* __restrict__ parts) {
+  constexpr int kAhead = 8;
+  const NormEntry e = t.e[table_entry(t.e, t.count, blockIdx.x)];
+  const int size = e.f32 ? 4 : 2;
+  const int64_t head = min(e.n, (int64_t)((16 - ((uintptr_t)e.data & 15)) & 15) / size);
+  const int64_t pieces = (e.n - head) * size / 16;
+  const uint4* p = reinterpret_cast<const uint4*>((const char*)e.data + head * size);
+  const int64_t q0 = (int64_t)(blockIdx.x - e.first) * (bytes / 16), q1 = min(pieces, q0 + bytes / 16);
   double sum = 0;
-  for (int64_t i = i0 + threadIdx.x; i < i1; i += 256) {
-    const double x = load_elem(e.data, i, e.f32);
-    sum += x * x;
+  for (int64_t q = q0 + threadIdx.x; q < q1; q += 256 * kAhead) {
+    uint4 a[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) a[k] = q + 256 * k < q1 ? p[q + 256 * k] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) sum += squares(a[k], e.f32);
+  }
+  if (blockIdx.x == e.first) {
+    const int64_t tail = head + pieces * 16 / size;
+    const int64_t i = threadIdx.x < 8 ? threadIdx.x : tail + threadIdx.x - 8;     // at most 7 on either side
+    if (threadIdx.x < 8 ? i < head : threadIdx.x < 16 && i < e.n) {
+      const double x = e.f32 ? ((const float*)e.data)[i] : bf16_to_f32(((const uint16_t*)e.data)[i]);
+      sum += x * x;
+    }
   }
   sum = block_sum_f64(sum);
   if (threadIdx.x == 0) parts[blockIdx.x] = sum;
@@ -227,10 +390,17 @@ lce_status_t check_adamw_tensor(const lce_adamw_tensor_t& t, int32_t n_groups, i
   return LCE_OK;
 }
 
-lce_status_t check_grads(const lce_grad_t* grads, int64_t count, int64_t* blocks) {
+inline int64_t norm_blocks(const lce_grad_t& g, int64_t bytes) {
+  return (g.n * (int64_t)dtype_bytes(g.dtype) + bytes - 1) / bytes;
+}
+
+// *bytes: what a workgroup of k_grad_squares takes, 32 KB (one round of loads) or as many times that as keep the
+// sums that the last workgroup adds near 4096 (1.2e9 bf16 elements: 75,000 sums took it 112 us);
+// *blocks: the workgroups, each tensor's rounded up
+lce_status_t check_grads(const lce_grad_t* grads, int64_t count, int64_t* bytes, int64_t* blocks) {
   if (count < 0) return LCE_ERR_SHAPE;
   if (count > 0 && !grads) return LCE_ERR_NULL;
-  *blocks = 0;
+  double total = 0;
   for (int64_t i = 0; i < count; ++i) {
     const lce_grad_t& g = grads[i];
     if (g.n < 0 || g.n >= kMostElems) return LCE_ERR_SHAPE;
@@ -238,8 +408,12 @@ lce_status_t check_grads(const lce_grad_t* grads, int64_t count, int64_t* blocks
     if (!known_dtype(g.dtype)) return LCE_ERR_UNSUPPORTED;
     if (g.n > 0 && !g.data) return LCE_ERR_NULL;
     if (!aligned(g.data, dtype_bytes(g.dtype))) return LCE_ERR_ALIGN;
-    *blocks += (g.n + kNormElems - 1) / kNormElems;
+    total += (double)g.n * dtype_bytes(g.dtype);
   }
+  *bytes = 32768;
+  while (total > 4096.0 * *bytes) *bytes *= 2;
+  *blocks = 0;
+  for (int64_t i = 0; i < count; ++i) *blocks += norm_blocks(grads[i], *bytes);
   return LCE_OK;
 }
 
@@ -289,7 +463,8 @@ lce_status_t lce_adamw_tensors_step(const lce_adamw_tensor_t* tensors, int64_t c
     }
     t.e[t.count++] = AdamWEntry{x.param, x.grad, x.exp_avg, x.exp_avg_sq, (uint8_t*)x.units, x.master, x.n,
                                 (uint32_t)blocks, (uint32_t)((uint64_t)x.place >> 1), (uint8_t)g,
-                                (uint8_t)(x.param_dtype == LCE_DTYPE_F32), (uint8_t)(x.grad_dtype == LCE_DTYPE_F32), {}};
+                                (uint8_t)(x.param_dtype == LCE_DTYPE_F32), (uint8_t)(x.grad_dtype == LCE_DTYPE_F32),
+                                (uint8_t)(aligned16(x.param) | aligned16(x.grad) << 1 | aligned16(x.master) << 2)};
     blocks += nb;
   }
   flush();
@@ -304,17 +479,17 @@ lce_status_t lce_adamw_moments(int64_t n, const void* exp_avg, const void* exp_a
   if (!aligned16(exp_avg) || !aligned16(exp_avg_sq) || !aligned(units, 2) || !aligned16(first) || !aligned16(root))
     return LCE_ERR_ALIGN;
   Launcher L{(hipStream_t)stream};
-  for (int64_t i = 0; i < n; i += 256 * kMostBlocks) {
-    const int64_t k = std::min<int64_t>(n - i, 256 * kMostBlocks);
-    L(K_ADAMW_MOMENTS, k_adamw_moments, dim3((unsigned)((k + 255) / 256)), dim3(256), k, (const uint8_t*)exp_avg + i,
+  for (int64_t i = 0; i < n; i += 2048 * kMostBlocks) {
+    const int64_t k = std::min<int64_t>(n - i, 2048 * kMostBlocks);
+    L(K_ADAMW_MOMENTS, k_adamw_moments, dim3((unsigned)((k + 2047) / 2048)), dim3(256), k, (const uint8_t*)exp_avg + i,
       (const uint8_t*)exp_avg_sq + i, (const uint8_t*)units + i / 16, (uint16_t*)first + i, (uint16_t*)root + i);
   }
   return L.st;
 }
 
 lce_status_t lce_grad_norm_workspace_size(const lce_grad_t* grads, int64_t count, size_t* bytes) {
-  int64_t blocks;
-  const lce_status_t st = check_grads(grads, count, &blocks);
+  int64_t per, blocks;
+  const lce_status_t st = check_grads(grads, count, &per, &blocks);
   if (st != LCE_OK) return st;
   if (!bytes) return LCE_ERR_NULL;
   *bytes = (size_t)round_up(8 * std::max<int64_t>(blocks, 1), 256);
@@ -323,8 +498,8 @@ lce_status_t lce_grad_norm_workspace_size(const lce_grad_t* grads, int64_t count
 
 lce_status_t lce_grad_norm(const lce_grad_t* grads, int64_t count, float max_norm, float* norm, float* factor,
                            void* workspace, size_t workspace_bytes, void* stream) {
-  int64_t blocks;
-  const lce_status_t st = check_grads(grads, count, &blocks);
+  int64_t bytes, blocks;
+  const lce_status_t st = check_grads(grads, count, &bytes, &blocks);
   if (st != LCE_OK) return st;
   if (!(max_norm > 0.f)) return LCE_ERR_ARG;
   if (!norm || !workspace) return LCE_ERR_NULL;
@@ -337,14 +512,14 @@ lce_status_t lce_grad_norm(const lce_grad_t* grads, int64_t count, float max_nor
   t.count = 0;
   const auto flush = [&] {
     if (t.count == 0) return;
-    L(K_GRAD_NORM, k_grad_squares, dim3((unsigned)here), dim3(256), t, parts + done);
+    L(K_GRAD_NORM, k_grad_squares, dim3((unsigned)here), dim3(256), t, bytes, parts + done);
     done += here;
     here = t.count = 0;
   };
   for (int64_t i = 0; i < count; ++i) {
     const lce_grad_t& g = grads[i];
     if (g.n == 0) continue;
-    const int64_t nb = (g.n + kNormElems - 1) / kNormElems;
+    const int64_t nb = norm_blocks(g, bytes);
     if (t.count == kNormTensors || here + nb > kMostBlocks) flush();
     t.e[t.count++] = NormEntry{g.data, g.n, (uint32_t)here, (uint32_t)(g.dtype == LCE_DTYPE_F32)};
     here += nb;
