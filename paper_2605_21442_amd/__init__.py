@@ -16,5 +16,6 @@ __all__ = ["linear_cross_entropy", "LinearCrossEntropy", "AdamWState", "linear_k
 def __getattr__(name):
     if name in __all__:
         from . import autograd, training
-        return getattr(autograd if hasattr(autograd, name) else training, name)
+        value = globals()[name] = getattr(autograd if hasattr(autograd, name) else training, name)
+        return value
     raise AttributeError(name)

@@ -301,12 +301,15 @@ struct NormTable {
 };
 static_assert(sizeof(NormTable) <= 4000, "launch arguments");
 
+template <int kThreads>
 __device__ __forceinline__ double block_sum_f64(double x) {
-  __shared__ double part[4];
+  __shared__ double part[kThreads / 64];
   for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
   __syncthreads();
-  return (part[0] + part[1]) + (part[2] + part[3]);
+  x = part[0];
+  for (int k = 1; k < kThreads / 64; ++k) x += part[k];
+  return x;
 }
 
 __device__ __forceinline__ double squares(const uint4 a, bool f32) {
@@ -352,15 +355,21 @@ __global__ __launch_bounds__(256) void k_grad_squares(NormTable t, int64_t bytes
       sum += x * x;
     }
   }
-  sum = block_sum_f64(sum);
+  sum = block_sum_f64<256>(sum);
   if (threadIdx.x == 0) parts[blockIdx.x] = sum;
 }
 
-__global__ __launch_bounds__(256) void k_grad_norm(const double* __restrict__ parts, int64_t count, float max_norm,
-                                                   float* norm, float* factor) {
+__global__ __launch_bounds__(1024) void k_grad_norm(const double* __restrict__ parts, int64_t count, float max_norm,
+                                                    float* norm, float* factor) {
   double sum = 0;
-  for (int64_t i = threadIdx.x; i < count; i += 256) sum += parts[i];
-  sum = block_sum_f64(sum);
+  for (int64_t i = threadIdx.x; i < count; i += 1024 * 8) {
+    double x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = i + 1024 * k < count ? parts[i + 1024 * k] : 0.0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += x[k];
+  }
+  sum = block_sum_f64<1024>(sum);
   if (threadIdx.x != 0) return;
   const double x = sqrt(sum), f = (double)max_norm / (x + 1e-6);
   *norm = (float)x;
@@ -395,7 +404,7 @@ inline int64_t norm_blocks(const lce_grad_t& g, int64_t bytes) {
 }
 
 // *bytes: what a workgroup of k_grad_squares takes, 32 KB (one round of loads) or as many times that as keep the
-// sums that the last workgroup adds near 4096 (1.2e9 bf16 elements: 75,000 sums took it 112 us);
+// sums that the last workgroup adds near 16384 (1.2e9 bf16 elements: 75,000 sums took it 112 us);
 // *blocks: the workgroups, each tensor's rounded up
 lce_status_t check_grads(const lce_grad_t* grads, int64_t count, int64_t* bytes, int64_t* blocks) {
   if (count < 0) return LCE_ERR_SHAPE;
@@ -411,7 +420,7 @@ lce_status_t check_grads(const lce_grad_t* grads, int64_t count, int64_t* bytes,
     total += (double)g.n * dtype_bytes(g.dtype);
   }
   *bytes = 32768;
-  while (total > 4096.0 * *bytes) *bytes *= 2;
+  while (total > 16384.0 * *bytes) *bytes *= 2;
   *blocks = 0;
   for (int64_t i = 0; i < count; ++i) *blocks += norm_blocks(grads[i], *bytes);
   return LCE_OK;
@@ -525,7 +534,7 @@ lce_status_t lce_grad_norm(const lce_grad_t* grads, int64_t count, float max_nor
     here += nb;
   }
   flush();
-  L(K_GRAD_NORM, k_grad_norm, dim3(1), dim3(256), (const double*)parts, blocks, max_norm, norm, factor);
+  L(K_GRAD_NORM, k_grad_norm, dim3(1), dim3(1024), (const double*)parts, blocks, max_norm, norm, factor);
   return L.st;
 }
 

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import contextlib
 import math
+import operator
 
 import numpy as np
 import torch
@@ -46,7 +47,7 @@ def _ids(ids: torch.Tensor, dev: torch.device) -> torch.Tensor:
         raise TypeError(f"ids must be int32 or int64, got {ids.dtype}")
     if ids.device != dev:
         raise ValueError(f"ids are on {ids.device}, the other operand on {dev}")
-    return ids.reshape(-1).contiguous()
+    return ids if ids.dim() == 1 and ids.is_contiguous() else ids.reshape(-1).contiguous()
 
 
 def embedding_forward(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0, padding_idx: int | None = None,
@@ -121,6 +122,8 @@ def token_embedding(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0,
     """``scale * weight[ids]``: the token embedding, with a gradient for the weight [V, D] (bf16 or fp32). Tokens
     of ``padding_idx`` give no gradient. An id outside the vocabulary gives a row of zeros and no gradient
     (``embedding_forward`` also reports it)."""
+    if not (weight.requires_grad and torch.is_grad_enabled()):
+        return embedding_forward(ids, weight, scale, padding_idx, want_status=False)[0]
     return TokenEmbedding.apply(ids, weight, scale, padding_idx)
 
 
@@ -129,31 +132,35 @@ def token_embedding(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0,
 _GRAD = np.dtype([("data", "u8"), ("n", "i8"), ("dtype", "i4"), ("reserved", "i4")])
 
 
-def _dense(grads, dev_index: int | None):
-    """The given tensors, contiguous, all on one device: (tensors, device index). What is not so is copied, or refused."""
-    for g in grads:
-        if g.dtype not in _DTYPES:
-            raise TypeError(f"gradients must be bfloat16 or float32, got {g.dtype}")
-        if not g.is_cuda:
-            raise ValueError("gradients must be GPU tensors")
-    where = {g.get_device() for g in grads} | ({dev_index} if dev_index is not None else set())
-    if len(where) > 1:
-        raise ValueError("gradients must be on one device")
-    return [g.contiguous() for g in grads]
+_dtype_of, _shape_of = operator.attrgetter("dtype"), operator.attrgetter("shape")
+
+
+def _dense(grads: list, dev_index: int | None) -> tuple[list, list]:
+    """(the given tensors, contiguous; their lce_dtype_t): what is not contiguous is copied, other types and several
+    devices are refused. A model has hundreds of tensors, so each property is read in one pass over all."""
+    dtypes = list(map(_dtype_of, grads))
+    if not set(dtypes) <= _DTYPES.keys():
+        raise TypeError(f"gradients must be bfloat16 or float32, got {set(dtypes) - _DTYPES.keys()}")
+    where = set(map(torch.Tensor.get_device, grads))
+    if -1 in where or len(where) > 1 or (dev_index is not None and where and where != {dev_index}):
+        raise ValueError("gradients must be GPU tensors on one device")
+    if not all(map(torch.Tensor.is_contiguous, grads)):
+        grads = [g.contiguous() for g in grads]
+    return grads, list(map(_DTYPES.__getitem__, dtypes))
 
 
 def grad_norm(grads, max_norm: float = math.inf) -> tuple[torch.Tensor, torch.Tensor]:
     """(norm, factor), fp32 scalars on the device, from lce_grad_norm: the norm of all tensors of ``grads``
     together (None entries are left out) and ``min(1, max_norm / (norm + 1e-6))``, for ``AdamWTensors.step``'s
     ``grad_scale``. The factor is NaN where the norm is not finite. Nothing waits for the device."""
-    grads = _dense([g for g in grads if g is not None], None)
+    grads, dtypes = _dense([g for g in grads if g is not None], None)
     if not grads:
         raise ValueError("no gradients")
     dev = grads[0].device
     t = np.zeros(len(grads), dtype=_GRAD)
-    t["data"] = [g.data_ptr() for g in grads]
-    t["n"] = [g.numel() for g in grads]
-    t["dtype"] = [_DTYPES[g.dtype] for g in grads]
+    t["data"] = list(map(torch.Tensor.data_ptr, grads))
+    t["n"] = list(map(torch.Tensor.numel, grads))
+    t["dtype"] = dtypes
     addr = t.ctypes.data
     nbytes = B.lce_grad_norm_workspace_size(addr, len(grads))
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
@@ -255,7 +262,7 @@ class AdamWTensors:
         changes but ``step_count``. ``seed``: 32 bits for the rounding of 8-bit moments, by default from the
         state's seed and the step."""
         params = self.params
-        if [p.data_ptr() for p in params] != self._addresses:
+        if list(map(torch.Tensor.data_ptr, params)) != self._addresses:
             raise ValueError("a parameter's storage has changed since the state was made")
         grads = [p.grad for p in params] if grads is None else list(grads)
         if len(grads) != len(params):
@@ -264,20 +271,21 @@ class AdamWTensors:
                                        or grad_scale.device != self.device):
             raise ValueError("grad_scale must be a one-element float32 tensor on the parameters' device")
         t = self._table.copy()
-        if any(g is None for g in grads):
-            t["n"][[g is None for g in grads]] = 0
-        shapes = [s if g is None else g.shape for g, s in zip(grads, self._shapes)]
-        if shapes != self._shapes:
+        have = [k for k, g in enumerate(grads) if g is not None]
+        shapes = self._shapes
+        if len(have) < len(grads):
+            grads, shapes = [grads[k] for k in have], [shapes[k] for k in have]
+            t = t[have]                            # (a copy: the tensors without a gradient are not in the call)
+        if list(map(_shape_of, grads)) != shapes:
             raise ValueError("gradients must be shaped like their parameters")
-        have = iter(_dense([g for g in grads if g is not None], self.device.index))
-        dense = [None if g is None else next(have) for g in grads]
-        t["grad"] = [0 if g is None else g.data_ptr() for g in dense]
-        t["grad_dtype"] = [0 if g is None else _DTYPES[g.dtype] for g in dense]
+        grads, dtypes = _dense(grads, self.device.index)
+        t["grad"] = list(map(torch.Tensor.data_ptr, grads))
+        t["grad_dtype"] = dtypes
         step = self.step_count + 1
         opts = (B.LceAdamW * len(self.groups))(*(
             B.adamw(g["lr"], g["betas"][0], g["betas"][1], g["eps"], g["weight_decay"], step) for g in self.groups))
         with _on(self.device):
-            B.lce_adamw_tensors_step(t.ctypes.data, len(params), opts, len(opts), self.state_bits,
+            B.lce_adamw_tensors_step(t.ctypes.data, len(t), opts, len(opts), self.state_bits,
                                      grad_scale.data_ptr() if grad_scale is not None else 0,
                                      self._seed_of(step) if seed is None else seed, _stream(self.device))
         self.step_count = step
