@@ -157,7 +157,8 @@ __global__ __launch_bounds__(1024) void k_embed_sort(EmbedRows e, int nb_log2, i
 }
 
 // ---------------------------------------------------------------------------------------------
-// Lookup: 16 bytes of a row per thread and step.
+// Lookup: a workgroup writes 8192 consecutive elements of out, a thread 8 of every 2048 of them, so that the rows of four
+// pieces are in flight and the stores go in the order of the addresses.
 // ---------------------------------------------------------------------------------------------
 template <typename T> struct Row8;      // 8 elements as fp32
 template <> struct Row8<uint16_t> {
@@ -197,22 +198,33 @@ struct EmbedIds {
 template <typename T>
 __global__ __launch_bounds__(256) void k_embed_lookup(EmbedIds e, int64_t v_total, const T* __restrict__ W, int64_t ldw,
                                                       int d, float scale, T* __restrict__ out, int* status) {
-  const int cpr = d >> 3;
-  const int64_t total = e.n * cpr;
-  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
-    const int64_t i = q / cpr;
-    const int col = (int)(q - i * cpr) * 8;
-    const int64_t id = load_target(e.ids, e.bytes, i);
-    const int64_t r = id - e.v_begin;
-    float x[8] = {};
-    if (id >= e.v_begin && r < e.v) {
-      Row8<T>::load(W + r * ldw + col, x);
+  constexpr int kAhead = 4;
+  const uint32_t row8 = (uint32_t)d >> 3;
+  for (int64_t block = blockIdx.x; block * (256 * kAhead) < e.n * row8; block += gridDim.x) {
+    const int64_t i0 = block * (256 * kAhead) / row8;
+    const uint32_t o0 = (uint32_t)(block * (256 * kAhead) - i0 * row8);
+    int64_t i[kAhead], id[kAhead];
+    uint32_t col[kAhead];
+    float x[kAhead][8] = {};
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] *= scale;
-    } else if (status && (id < 0 || id >= v_total) && id != e.padding) {
-      *status = LCE_STATUS_ID_OUT_OF_RANGE;   // every writer writes the same value
+    for (int k = 0; k < kAhead; ++k) {
+      const uint32_t o = o0 + threadIdx.x + 256 * k;
+      i[k] = i0 + o / row8;
+      col[k] = o % row8 * 8;
+      id[k] = load_target(e.ids, e.bytes, min(i[k], e.n - 1));
     }
-    Row8<T>::store(out + i * d + col, x);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (id[k] >= e.v_begin && id[k] - e.v_begin < e.v) Row8<T>::load(W + (id[k] - e.v_begin) * ldw + col[k], x[k]);
+      else if (status && (id[k] < 0 || id[k] >= v_total) && id[k] != e.padding)
+        *status = LCE_STATUS_ID_OUT_OF_RANGE;   // every writer writes the same value
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (i[k] >= e.n) break;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) x[k][c] *= scale;
+      Row8<T>::store(out + i[k] * d + col[k], x[k]);
+    }
   }
 }
 
@@ -419,7 +431,7 @@ lce_status_t make_embed_plan(const lce_embedding_t* p, EmbedPlan* pl) {
 template <typename T>
 void launch_lookup(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedIds& e, const void* W, void* out,
                    int32_t* status) {
-  const int64_t blocks = (p->n * (p->d / 8) + 255) / 256;
+  const int64_t blocks = (p->n * (p->d / 8) + 1023) / 1024;
   L(K_EMBED_LOOKUP, k_embed_lookup<T>, dim3((unsigned)std::min<int64_t>(blocks, 1 << 20)), dim3(256), e, pl.v_total,
     (const T*)W, pl.ldw, (int)p->d, p->scale, (T*)out, status);
 }
