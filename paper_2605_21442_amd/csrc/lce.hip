@@ -134,6 +134,11 @@ __device__ __forceinline__ void store16_padded(void* p, i32x4_t v) {
   asm volatile("global_store_dwordx4 %0, %1, off\n\ts_nop 7" : : "v"(p), "v"(v) : "memory");
 }
 
+// The same, passing the L2 without displacing what is there, for data that is written once and far larger than it.
+__device__ __forceinline__ void store16_padded_nt(void* p, i32x4_t v) {
+  asm volatile("global_store_dwordx4 %0, %1, off nt\n\ts_nop 7" : : "v"(p), "v"(v) : "memory");
+}
+
 // The same for a 16-byte store through a buffer resource (descriptor words rw, per-lane voffset,
 // uniform soffset).
 __device__ __forceinline__ void buffer_store16_padded(i32x4_t v, const i32x4_t& rw, uint32_t voffset,
