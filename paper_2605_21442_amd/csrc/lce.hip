@@ -185,20 +185,13 @@ struct AdamWState {
   float* master;
 };
 
-// One element's update; returns the root of the new v.
-__device__ __forceinline__ float adamw_update_root(float& p, float& m, float& v, float g, const AdamWConst& c) {
+__device__ __forceinline__ void adamw_update(float& p, float& m, float& v, float g, const AdamWConst& c) {
 #pragma clang fp contract(off)
   p = p * c.keep;
   m = c.beta1 * m + c.omb1 * g;
   v = c.beta2 * v + c.omb2 * (g * g);
-  const float root = sqrtf(v);
-  const float denom = root * c.inv_sqrt_bc2 + c.eps;
+  const float denom = sqrtf(v) * c.inv_sqrt_bc2 + c.eps;
   p = p - c.step_size * (m / denom);
-  return root;
-}
-
-__device__ __forceinline__ void adamw_update(float& p, float& m, float& v, float g, const AdamWConst& c) {
-  (void)adamw_update_root(p, m, v, g, c);
 }
 
 __device__ __forceinline__ int64_t load_target(const void* t, int tbytes, int64_t i) {
