@@ -29,6 +29,7 @@ struct AdamWTable {
   AdamWEntry e[kTableTensors];
   AdamWConst g[kTableGroups];
   int count;
+  int per;                 // elements of a workgroup, a multiple of 2048 (whole rounds of either form)
 };
 static_assert(sizeof(AdamWTable) <= 4000, "launch arguments");
 
@@ -170,9 +171,6 @@ __device__ __forceinline__ float adamw_update_near(float& p, float& m, float r, 
   return root;
 }
 
-constexpr int kStepElems = 8192;       // elements of a workgroup
-static_assert(kStepElems % 2048 == 0, "whole rounds of either form");
-
 // 32-bit moments: 4 elements per thread and round, so that every access of a wave is contiguous.
 __device__ __forceinline__ void adamw_round32(const AdamWEntry& e, const AdamWConst& c, int64_t i, float scale, bool scaled) {
 #pragma clang fp contract(off)
@@ -268,8 +266,8 @@ __global__ __launch_bounds__(256) void k_adamw_tensors(AdamWTable t, const float
   const AdamWEntry e = t.e[table_entry(t.e, t.count, blockIdx.x)];
   const AdamWConst c = t.g[e.group];
   constexpr int kPer = kBits == 32 ? 4 : 8;
-  const int64_t i0 = (int64_t)(blockIdx.x - e.first) * kStepElems;
-  for (int j = 0; j < kStepElems && i0 + j < e.n; j += 256 * kPer) {
+  const int64_t i0 = (int64_t)(blockIdx.x - e.first) * t.per;
+  for (int j = 0; j < t.per && i0 + j < e.n; j += 256 * kPer) {
     const int64_t i = i0 + j + kPer * threadIdx.x;
     if constexpr (kBits == 32) {
       if (i < e.n) adamw_round32(e, c, i, scale, grad_scale != nullptr);
@@ -459,10 +457,17 @@ lce_status_t lce_adamw_tensors_step(const lce_adamw_tensor_t* tensors, int64_t c
   AdamWConst c;
   for (int32_t g = 0; g < n_groups; ++g)
     if (const lce_status_t st = make_adamw(&groups[g], &c); st != LCE_OK) return st;
-  for (int64_t i = 0; i < count; ++i)
+  int64_t total = 0;
+  for (int64_t i = 0; i < count; ++i) {
     if (const lce_status_t st = check_adamw_tensor(tensors[i], n_groups, state_bits); st != LCE_OK) return st;
+    total += tensors[i].n;
+  }
   Launcher L{(hipStream_t)stream};
   AdamWTable t;
+  // elements of a workgroup: 2048, for enough workgroups to fill the card, or up to 8192 where there are more than
+  // 4096 of them, each of which first finds its tensor
+  t.per = 2048;
+  while (t.per < 8192 && total > (int64_t)4096 * t.per) t.per *= 2;
   int32_t group_of[kTableGroups];
   int n_table_groups = 0;
   int64_t blocks = 0;
@@ -477,7 +482,7 @@ lce_status_t lce_adamw_tensors_step(const lce_adamw_tensor_t* tensors, int64_t c
   for (int64_t i = 0; i < count; ++i) {
     const lce_adamw_tensor_t& x = tensors[i];
     if (x.n == 0) continue;
-    const int64_t nb = (x.n + kStepElems - 1) / kStepElems;
+    const int64_t nb = (x.n + t.per - 1) / t.per;
     int g = 0;
     while (g < n_table_groups && group_of[g] != x.group) ++g;
     if (t.count == kTableTensors || g == kTableGroups || blocks + nb > kMostBlocks) {
