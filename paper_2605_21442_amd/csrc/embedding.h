@@ -161,11 +161,13 @@ __global__ __launch_bounds__(1024) void k_embed_sort(EmbedRows e, int nb_log2, i
 // pieces are in flight and the stores go in the order of the addresses. They pass the L2 by: kept there, they push out the
 // rows of frequent ids, which are read again and again (32768 tokens of 3584: 82 against 49 us; 16384 of 4096: 42 against 29).
 // ---------------------------------------------------------------------------------------------
-template <typename T> struct Row8;      // 8 elements as fp32
+// 8 elements: as they lie in memory (so that a load is only issued where it stands), and as fp32
+template <typename T> struct Row8;
 template <> struct Row8<uint16_t> {
-  static __device__ __forceinline__ void load(const uint16_t* p, float x[8]) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+  struct Raw { uint4 a; };
+  static __device__ __forceinline__ Raw fetch(const uint16_t* p) { return {*reinterpret_cast<const uint4*>(p)}; }
+  static __device__ __forceinline__ void unpack(const Raw& r, float x[8]) {
+    const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
 #pragma unroll
     for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
   }
@@ -178,9 +180,12 @@ template <> struct Row8<uint16_t> {
   }
 };
 template <> struct Row8<float> {
-  static __device__ __forceinline__ void load(const float* p, float x[8]) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  struct Raw { float4 a, b; };
+  static __device__ __forceinline__ Raw fetch(const float* p) {
+    return {*reinterpret_cast<const float4*>(p), *reinterpret_cast<const float4*>(p + 4)};
+  }
+  static __device__ __forceinline__ void unpack(const Raw& r, float x[8]) {
+    x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w; x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
   }
   template <bool kOnce = false>
   static __device__ __forceinline__ void store(float* p, const float x[8]) {
@@ -211,7 +216,8 @@ __global__ __launch_bounds__(256) void k_embed_lookup(EmbedIds e, int64_t v_tota
     const uint32_t o0 = (uint32_t)(block * (256 * kAhead) - i0 * row8);
     int64_t i[kAhead], id[kAhead];
     uint32_t col[kAhead];
-    float x[kAhead][8] = {};
+    bool held[kAhead];
+    typename Row8<T>::Raw raw[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const uint32_t o = o0 + threadIdx.x + 256 * k;
@@ -220,16 +226,23 @@ __global__ __launch_bounds__(256) void k_embed_lookup(EmbedIds e, int64_t v_tota
       id[k] = load_target(e.ids, e.bytes, min(i[k], e.n - 1));
     }
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      if (id[k] >= e.v_begin && id[k] - e.v_begin < e.v) Row8<T>::load(W + (id[k] - e.v_begin) * ldw + col[k], x[k]);
-      else if (status && (id[k] < 0 || id[k] >= v_total) && id[k] != e.padding)
-        *status = LCE_STATUS_ID_OUT_OF_RANGE;   // every writer writes the same value
+    for (int k = 0; k < kAhead; ++k) {          // (an id that W does not hold reads row 0, which is then not used)
+      held[k] = id[k] >= e.v_begin && id[k] - e.v_begin < e.v;
+      raw[k] = Row8<T>::fetch(W + (held[k] ? id[k] - e.v_begin : 0) * ldw + col[k]);
+    }
+    if (status)
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if ((id[k] < 0 || id[k] >= v_total) && id[k] != e.padding)
+          *status = LCE_STATUS_ID_OUT_OF_RANGE;   // every writer writes the same value
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       if (i[k] >= e.n) break;
+      float x[8];
+      Row8<T>::unpack(raw[k], x);
 #pragma unroll
-      for (int c = 0; c < 8; ++c) x[k][c] *= scale;
-      Row8<T>::template store<true>(out + i[k] * d + col[k], x[k]);
+      for (int c = 0; c < 8; ++c) x[c] = held[k] ? x[c] * scale : 0.f;
+      Row8<T>::template store<true>(out + i[k] * d + col[k], x);
     }
   }
 }
@@ -253,10 +266,11 @@ struct EmbedSorted {
   __device__ __forceinline__ int count() const { return starts[(int64_t)rows << nb_log2]; }
 };
 
+// (old: what dW holds there, where the sum is added to it)
 template <typename TW, bool kAdd>
-__device__ __forceinline__ void grad_store(TW* o, const float sum[8], float scale) {
+__device__ __forceinline__ void grad_store(TW* o, const typename Row8<TW>::Raw& old, const float sum[8], float scale) {
   float x[8] = {};
-  if (kAdd) Row8<TW>::load(o, x);
+  if (kAdd) Row8<TW>::unpack(old, x);
 #pragma unroll
   for (int k = 0; k < 8; ++k) x[k] += scale * sum[k];
   Row8<TW>::store(o, x);
@@ -271,47 +285,56 @@ __global__ __launch_bounds__(256) void k_embed_grad(EmbedSorted s, const T* __re
   const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   if (unit >= chunk_units) return;
   const int chunk = (int)(unit / slices);
-  const int col = (int)(unit - (int64_t)chunk * slices) * kGradCols + lane * 8;
-  const bool live = col < d;
+  const int col0 = (int)(unit - (int64_t)chunk * slices) * kGradCols + lane * 8;
+  const bool live = col0 < d;
+  const int col = live ? col0 : 0;             // (lanes behind the row read its start and store nothing)
   const int nv = s.count();
   const int c0 = chunk * per, c1 = min(nv, c0 + per);
   if (c0 >= c1) return;
   const int before = c0 > 0 ? s.pairs[c0 - 1].x : -1, after = c1 < nv ? s.pairs[c1].x : -1;
   float* part = parts + (int64_t)chunk * 2 * d + col;
   float sum[8] = {};
-  int cur = s.pairs[c0].x;
   bool first = true;               // still at the chunk's first id
-  const auto flush = [&](bool last) {
-    const bool from_before = first && cur == before, goes_on = last && cur == after;
-    first = false;
-    if (!live) return;
-    if (from_before || goes_on) Row8<float>::store(part + (from_before ? 0 : d), sum);
-    else grad_store<TW, kAdd>(dw + (int64_t)cur * d + col, sum, scale);
-  };
   for (int g0 = c0; g0 < c1; g0 += 64) {
     const int here = min(64, c1 - g0);
-    const int2 my = lane < here ? s.pairs[g0 + lane] : make_int2(-1, 0);
+    const int2 my = s.pairs[g0 + min(lane, here - 1)];
+    const int next = __shfl_down(my.x, 1);     // the id behind; at the group's end the next group's, or `after`
+    const int follow = lane < here - 1 ? next : g0 + here < c1 ? s.pairs[g0 + here].x : after;
+    const unsigned long long ends = __ballot(my.x != follow || (g0 + lane == c1 - 1));
     for (int p = 0; p < here; p += kAhead) {
-      float x[kAhead][8] = {};
+      // the rows of dOut, and of dW where an id ends, all in flight
+      typename Row8<T>::Raw x[kAhead];
+      typename Row8<TW>::Raw old[kAhead];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        if (p + k < here && live) Row8<T>::load(dout + (int64_t)__builtin_amdgcn_readlane(my.y, p + k) * ldx + col, x[k]);
+      for (int k = 0; k < kAhead; ++k) {
+        const int q = min(p + k, here - 1);
+        x[k] = Row8<T>::fetch(dout + (int64_t)__builtin_amdgcn_readlane(my.y, q) * ldx + col);
+      }
+      if constexpr (kAdd)
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          if ((ends >> min(p + k, 63)) & 1)
+            old[k] = Row8<TW>::fetch(dw + (int64_t)__builtin_amdgcn_readlane(my.x, min(p + k, here - 1)) * d + col);
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         if (p + k >= here) break;
-        const int r = __builtin_amdgcn_readlane(my.x, p + k);
-        if (r != cur) {
-          flush(false);
-          cur = r;
+        float y[8];
+        Row8<T>::unpack(x[k], y);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+        for (int e = 0; e < 8; ++e) sum[e] += y[e];
+        if (((ends >> (p + k)) & 1) == 0) continue;
+        const int r = __builtin_amdgcn_readlane(my.x, p + k);
+        const bool from_before = first && r == before, goes_on = g0 + p + k == c1 - 1 && r == after;
+        first = false;
+        if (live) {
+          if (from_before || goes_on) Row8<float>::store(part + (from_before ? 0 : d), sum);
+          else grad_store<TW, kAdd>(dw + (int64_t)r * d + col, old[k], sum, scale);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] += x[k][e];
+        for (int e = 0; e < 8; ++e) sum[e] = 0.f;
       }
     }
   }
-  flush(true);
 }
 
 // The rows of a fresh dW without a token, in the order of the addresses: 16 KB of dW per workgroup, 16 bytes of each
@@ -361,16 +384,18 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedSorted s, int v, int d,
   const bool live = col < d;
   float sum[8] = {};
   if (live) {
-    if (w == 0) Row8<float>::load(parts + ((int64_t)chunk * 2 + 1) * d + col, sum);
+    if (w == 0) Row8<float>::unpack(Row8<float>::fetch(parts + ((int64_t)chunk * 2 + 1) * d + col), sum);
     for (int c = chunk + 1 + w; c <= last; c += 16) {
-      float x[4][8];
+      Row8<float>::Raw x[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) Row8<float>::load(parts + (int64_t)min(c + 4 * k, last) * 2 * d + col, x[k]);
+      for (int k = 0; k < 4; ++k) x[k] = Row8<float>::fetch(parts + (int64_t)min(c + 4 * k, last) * 2 * d + col);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (c + 4 * k <= last)
+      for (int k = 0; k < 4; ++k) {
+        float y[8];
+        Row8<float>::unpack(x[k], y);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum[e] += x[k][e];
+        for (int e = 0; e < 8; ++e) sum[e] += c + 4 * k <= last ? y[e] : 0.f;
+      }
     }
     if (w > 0)
 #pragma unroll
@@ -382,7 +407,10 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedSorted s, int v, int d,
   for (int k = 0; k < 3; ++k)
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += sums[k][e * 64 + lane];
-  grad_store<TW, kAdd>(dw + (int64_t)r * d + col, sum, scale);
+  TW* o = dw + (int64_t)r * d + col;
+  typename Row8<TW>::Raw old{};
+  if (kAdd) old = Row8<TW>::fetch(o);
+  grad_store<TW, kAdd>(o, old, sum, scale);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -422,11 +450,12 @@ lce_status_t make_embed_plan(const lce_embedding_t* p, EmbedPlan* pl) {
   size_t cur = 0;
   pl->o_sorted = take(cur, 8 * (size_t)p->n);
   pl->o_starts = take(cur, 4 * (((size_t)pl->rows << pl->nb_log2) + 1));
-  // tokens of a chunk: 8 to 64, for 4096 waves (16 per CU, each with eight rows' loads in flight); more where there
-  // would be more than 4096 chunks, whose two sums each bound the workspace
+  // tokens of a chunk: 8 to 64, for 4096 waves (16 per CU, each with eight rows' loads in flight), and in narrow rows no
+  // fewer than keep the chunks of a frequent id few for the join, which takes 16 of them a step as a wave takes 8 rows
+  // (65070 tokens of 88: 58 us with 16); more where there would be more than 4096 chunks, whose sums bound the workspace
   pl->slices = (int)((p->d + kGradCols - 1) / kGradCols);
   pl->per = 8;
-  while (pl->per < 64 && p->n * pl->slices > (int64_t)4096 * pl->per) pl->per *= 2;
+  while (pl->per < 64 && (p->n * pl->slices > (int64_t)4096 * pl->per || p->n > (int64_t)16 * pl->per * pl->per)) pl->per *= 2;
   while (p->n > (int64_t)4096 * pl->per) pl->per *= 2;
   pl->chunks = (p->n + pl->per - 1) / pl->per;
   pl->o_parts = take(cur, 8 * (size_t)pl->chunks * p->d);

@@ -22,9 +22,12 @@ from .autograd import _rows_usable, _stream
 _DTYPES = {torch.bfloat16: B.LCE_DTYPE_BF16, torch.float32: B.LCE_DTYPE_F32}
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on(dev: torch.device):
     """The tensors' device as the current one while a call is enqueued: its default stream has no device of its own."""
-    return contextlib.nullcontext() if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+    return _HERE if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
 
 
 # ---- token embedding ----------------------------------------------------------------------------
@@ -59,13 +62,16 @@ def embedding_forward(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.
         raise ValueError(f"weight must be [V, D], got {tuple(weight.shape)}")
     w, ldw = _rows(weight, "weight")
     t = _ids(ids, w.device)
-    p = B.embedding(t.numel(), w.shape[1], w.shape[0], ld_w=ldw, v_begin=v_begin, v_total=v_total,
-                    padding_idx=padding_idx, scale=scale, id_bytes=t.element_size(), dtype=_DTYPES[w.dtype])
-    out = torch.empty((*ids.shape, w.shape[1]), dtype=w.dtype, device=w.device)
-    status = torch.empty(1, dtype=torch.int32, device=w.device) if want_status else None
-    with _on(w.device):
-        B.lce_embedding_forward(p, w.data_ptr(), t.data_ptr(), out.data_ptr(),
-                                status.data_ptr() if want_status else 0, _stream(w.device))
+    v, d = w.shape
+    dev, kind = w.device, _DTYPES[w.dtype]
+    # (B.embedding's structure, in place: a lookup of few tokens is as long as the host takes for it)
+    p = B.LceEmbedding(t.numel(), d, v, ldw, 0, v_begin, v_total, B.LCE_NO_PADDING if padding_idx is None else padding_idx,
+                       scale, t.element_size(), kind, kind, 0, 0)
+    out = torch.empty((*ids.shape, d), dtype=w.dtype, device=dev)
+    status = torch.empty(1, dtype=torch.int32, device=dev) if want_status else None
+    with _on(dev):
+        B.lce_embedding_forward(p, w.data_ptr(), t.data_ptr(), out.data_ptr(), status.data_ptr() if want_status else 0,
+                                _stream(dev))
     return out, status
 
 
