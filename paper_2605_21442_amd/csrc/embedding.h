@@ -441,6 +441,8 @@ lce_status_t make_embed_plan(const lce_embedding_t* p, EmbedPlan* pl) {
   pl->ldx = p->ld_x ? p->ld_x : p->d;
   if (pl->ldw < p->d || pl->ldx < p->d || pl->ldw >= (int64_t)1 << 30 || pl->ldx >= (int64_t)1 << 30) return LCE_ERR_SHAPE;
   if (pl->ldw % 8 != 0 || pl->ldx % 8 != 0) return LCE_ERR_ALIGN;
+  // a launch takes fewer than 2^32 threads, and zeroes 16 KB of dW with 256 of them
+  if ((uint64_t)p->v * p->d * (p->dw_dtype == LCE_DTYPE_F32 ? 4 : 2) > (uint64_t)1 << 37) return LCE_ERR_SHAPE;
   // 256 buckets, one per CU, or as many as keep a bucket's counts in LDS; no more than there are ids
   pl->nb_log2 = 0;
   while (pl->nb_log2 < 8 && ((int64_t)1 << pl->nb_log2) < p->v) ++pl->nb_log2;

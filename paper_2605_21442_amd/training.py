@@ -15,6 +15,7 @@ import operator
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 from .autograd import _rows_usable, _stream
@@ -116,6 +117,7 @@ class TokenEmbedding(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad):
         (ids,) = ctx.saved_tensors
         v, scale, padding_idx = ctx.opts
@@ -266,7 +268,8 @@ class AdamWTensors:
         the parameters' ``.grad``; a tensor without one is left as it is, moments included. ``grad_scale``: an fp32
         GPU scalar that multiplies every gradient first (``grad_norm``'s factor); where it is not finite, nothing
         changes but ``step_count``. ``seed``: 32 bits for the rounding of 8-bit moments, by default from the
-        state's seed and the step."""
+        state's seed and the step. A step captured into a graph keeps the count, the rates and the seed that it
+        was captured with in every replay."""
         params = self.params
         if list(map(torch.Tensor.data_ptr, params)) != self._addresses:
             raise ValueError("a parameter's storage has changed since the state was made")

@@ -353,6 +353,19 @@ def test_norm_of_large_small_and_no_values():
     assert math.isnan(norm.item()) and math.isnan(factor.item())
 
 
+def test_norm_of_no_tensors_through_the_c_entry():
+    import torch
+    from paper_2605_21442_amd import binding as B
+    out = torch.full((2,), -1.0, device="cuda:0")
+    ws = torch.empty(B.lce_grad_norm_workspace_size(0, 0), dtype=torch.uint8, device="cuda:0")
+    B.lce_grad_norm(0, 0, 1.0, out.data_ptr(), out.data_ptr() + 4, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+    assert out.tolist() == [0.0, 1.0]
+    g = torch.ones(5, device="cuda:0")
+    t = (B.LceGrad * 1)(B.LceGrad(g.data_ptr(), 5, B.LCE_DTYPE_F32, 0))
+    B.lce_grad_norm(ctypes.addressof(t), 1, 1.0, out.data_ptr(), 0, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+    assert abs(out[0].item() - 5 ** 0.5) < 1e-6 and out[1].item() == 1.0      # no factor asked for: left alone
+
+
 def _step_of_a_small_model():
     """ids -> embedding -> two matrices -> loss -> gradients -> clipped AdamW, weights tied; returns a function that runs one
     step, what it changes, and the optimizer."""

@@ -235,6 +235,11 @@ def test_autograd_gives_the_formula_and_the_differences():
         # w + h and the scaled row round once each: 2^-24 of |w| + 1/2, times 3 |up|, twice
         assert abs((f[0] - f[1]) - float(ref[r, c])) <= 4 * 2.0 ** -23 * 3 * float((w.detach().abs().max() + 1) * up.abs().sum())
     assert token_embedding(ids, w.detach()).grad_fn is None
+    with torch.no_grad():
+        assert token_embedding(ids, w).grad_fn is None
+    (g,) = torch.autograd.grad(token_embedding(ids, w).square().sum(), w, create_graph=True)
+    with pytest.raises(RuntimeError):                   # no second derivative, and none taken for zero
+        g.sum().backward()
 
 
 def test_tied_weights_join_the_heads_gradient():

@@ -23,6 +23,7 @@ A, C, D, E, F, G, H = (0x100000 * k for k in range(1, 8))
     (dict(scale=float("nan")), B.LCE_ERR_ARG), (dict(scale=float("inf")), B.LCE_ERR_ARG),
     (dict(flags=B.LCE_FLAG_REUSE_FORWARD), B.LCE_ERR_ARG), (dict(flags=8), B.LCE_ERR_ARG),
     (dict(v_total=99), B.LCE_ERR_SHAPE), (dict(v_total=200, v_begin=101), B.LCE_ERR_SHAPE), (dict(v_begin=1), B.LCE_ERR_SHAPE),
+    (dict(v=1 << 29, d=512), B.LCE_ERR_SHAPE), (dict(v=1 << 18, d=1 << 18, dw_dtype=B.LCE_DTYPE_F32), B.LCE_ERR_SHAPE),
     (dict(v_total=200, v_begin=-1), B.LCE_ERR_SHAPE), (dict(v_begin=(1 << 63) - 1), B.LCE_ERR_SHAPE),
 ])
 def test_bad_embeddings_are_rejected(kw, code):
