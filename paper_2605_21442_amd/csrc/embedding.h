@@ -16,6 +16,10 @@ namespace {
 // token of every id, at which it then puts its tokens. A wave owns consecutive tokens, so the order within an id is
 // the tokens'. No workgroup waits for another, and counts do not depend on an order. A wave lists its tokens of the
 // bucket in LDS as it counts them, so only one with more than the list holds walks the ids twice.
+// 709 / 4096 / 16384 / 65070 tokens: 6.2 / 7.2 / 10.2 / 30 us. Short batches are bound by the chain of loads, barriers and the
+// scan; long ones by the vector instructions of the walk (every bucket looks at every id) in the bucket of the
+// most frequent id, half a microsecond per 1000 tokens. (Ranks by one ballot per bit for every group of 64 tokens, without
+// the lists: 22 us for 16384 tokens; ids loaded one group at a time: 30.)
 // ---------------------------------------------------------------------------------------------
 constexpr int kSortWaves = 16;
 constexpr int kSortIds = 1024;     // most ids of a bucket, one per thread in the scan
@@ -255,6 +259,8 @@ __global__ void k_embed_clear_status(int* status) { *status = 0; }
 // that reaches over a chunk's edge leaves an fp32 sum per chunk, in the chunk's slot 0 where it goes on from the chunk
 // before and in slot 1 where it starts, and k_embed_join adds these in the order of the chunks. So a frequent id
 // is spread over many waves, and the order of all sums follows from the ids and N alone.
+// Bound by memory: 4096 tokens added to a 128256 x 8192 dW 21.5 us (5.5 TB/s), 32768 to a 152064 x 3584 dW 64 us (4.6); one
+// workgroup per id, the simplest form, took 700 us for the former: the most frequent id's tokens came one after the other.
 // ---------------------------------------------------------------------------------------------
 constexpr int kGradCols = 512;     // columns of a wave
 

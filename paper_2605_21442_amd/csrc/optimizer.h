@@ -1,6 +1,12 @@
 // AdamW over many tensors (moments in 32 or 8 bits) and the norm of many gradients. Included by lce.hip,
 // behind its launcher. A launch serves up to kTableTensors tensors, whose addresses travel in its arguments: nothing
 // is copied to the device beforehand, so a call can be captured and its table needs no storage.
+//
+// All of it is bound by memory on a whole model (1.2e9 bf16 elements): the 32-bit step with an fp32 master copy moves
+// 28 bytes an element in 6.52 ms (5.3 TB/s), the 8-bit step without 10.1 bytes in 2.55 to 2.63 ms (4.8 TB/s; its vector
+// instructions alone would take 2.0), the values of the 8-bit moments 6.1 bytes in 1.3 ms (5.7), the norm 2 bytes in
+// 0.40 ms (6.1). Hundreds of small tensors are bound by the launches' ramps (224 adapter tensors, 7.9e6 elements: 81 us in 5
+// launches, 3.9 TB/s) and by the host that gathers their addresses.
 #pragma once
 
 namespace {
