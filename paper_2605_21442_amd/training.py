@@ -17,6 +17,7 @@ import operator
 import numpy as np
 import torch
 from torch.autograd.function import once_differentiable
+from torch.autograd.graph import increment_version
 
 from . import binding as B
 from .autograd import _rows_usable, _stream
@@ -104,6 +105,8 @@ def embedding_backward(ids: torch.Tensor, grad_out: torch.Tensor, v: int, scale:
     ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
     with _on(x.device):
         B.lce_embedding_backward(p, t.data_ptr(), x.data_ptr(), dw.data_ptr(), ws.data_ptr(), nbytes, _stream(x.device))
+    if accumulate_into is not None and not dw.is_inference():
+        increment_version(dw)
     return dw
 
 
@@ -266,6 +269,7 @@ class AdamWTensors:
         t["place"], t["group"] = off, at
         t["param_dtype"] = [_DTYPES[p.dtype] for p in self.params]
         self._table, self._addresses = t, t["param"].tolist()
+        self._tracked = [p for p in self.params if not p.is_inference()]
 
     def _seed_of(self, step: int) -> int:
         return (self.seed * 0x9E3779B9 + step * 0x6A09E667) & 0xFFFFFFFF
@@ -304,6 +308,7 @@ class AdamWTensors:
             B.lce_adamw_tensors_step(t.ctypes.data, len(t), opts, len(opts), self.state_bits,
                                      grad_scale.data_ptr() if grad_scale is not None else 0,
                                      self._seed_of(step) if seed is None else seed, _stream(self.device))
+        increment_version(self._tracked)       # a graph that saved a parameter before refuses its backward now
         self.step_count = step
 
     def moments(self) -> tuple[torch.Tensor, torch.Tensor]:

@@ -366,6 +366,61 @@ def test_norm_of_no_tensors_through_the_c_entry():
     assert abs(out[0].item() - 5 ** 0.5) < 1e-6 and out[1].item() == 1.0      # no factor asked for: left alone
 
 
+def test_a_step_between_forward_and_backward_is_noticed():
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    w, x = _draw((8, 8), 1).requires_grad_(), _draw((4, 8), 2).requires_grad_()
+    opt = AdamWTensors([w], **HP)
+    y = (x @ w).sum()
+    opt.step([torch.ones_like(w)])
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.backward()
+    with torch.inference_mode():
+        v = torch.zeros(8, device="cuda:0")
+        AdamWTensors([v], **HP).step([torch.ones(8, device="cuda:0")])
+        assert v.ne(0).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_elements_past_32_bit_offsets(bits):
+    # the last 5000 elements of a tensor of 2^32 + 77, against a call on them alone with the place they have there
+    import torch
+    from paper_2605_21442_amd import AdamWTensors, binding as B
+    n, tail = (1 << 32) + 77, 4992 + 77
+    at = n - tail                                   # a multiple of 32
+    print(f"case adamw n={n} {bits} bits", flush=True)
+    p = torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda:0")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda:0")
+    p[at:], g[at:] = _draw(tail, 3, 0.5, torch.bfloat16), _draw(tail, 4, 0.1, torch.bfloat16)
+    q, h = p[at:].clone(), g[at:].clone()
+    opt = AdamWTensors([p], state_bits=bits, **HP)
+    opt.step([g], seed=6)
+    kind = torch.float32 if bits == 32 else torch.uint8
+    size = -(-tail // 32) * 32
+    m, v, u = (torch.zeros(size, dtype=kind, device="cuda:0"), torch.zeros(size, dtype=kind, device="cuda:0"),
+               torch.zeros(size // 32, 2, dtype=torch.uint8, device="cuda:0"))
+    t = (B.LceAdamWTensor * 1)(B.LceAdamWTensor(q.data_ptr(), h.data_ptr(), m.data_ptr(), v.data_ptr(),
+                                                u.data_ptr() if bits == 8 else None, None, tail, at, 0, 0, 0, 0))
+    o = (B.LceAdamW * 1)(B.adamw(HP["lr"], *HP["betas"], HP["eps"], HP["weight_decay"], 1))
+    B.lce_adamw_tensors_step(ctypes.addressof(t), 1, ctypes.addressof(o), 1, bits, 0, 6, torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(p[at:], q) and torch.equal(opt.exp_avg[at:n], m[:tail])
+    assert torch.equal(opt.exp_avg_root[at:n] if bits == 8 else opt.exp_avg_sq[at:n], v[:tail])
+    assert bool((p[:64] == p[0]).all()) and bool((p[at - 64:at] == p[0]).all())       # zero gradients: decayed alike
+    if bits == 8:
+        first, root = opt.moments()
+        assert torch.equal(opt.units[at // 32:], u) and not first[at - 64:at].any() and first[at:].any()
+
+
+def test_norm_past_32_bit_offsets():
+    import torch
+    from paper_2605_21442_amd import grad_norm
+    n = (1 << 32) + 77
+    g = torch.ones(n, dtype=torch.bfloat16, device="cuda:0")
+    assert grad_norm([g])[0].item() == np.float32(math.sqrt(n))
+    g[-1] = 2.0 ** 20
+    assert grad_norm([g])[0].item() == np.float32(math.sqrt(n - 1 + 2.0 ** 40))
+
+
 def _step_of_a_small_model():
     """ids -> embedding -> two matrices -> loss -> gradients -> clipped AdamW, weights tied; returns a function that runs one
     step, what it changes, and the optimizer."""

@@ -331,3 +331,31 @@ def test_rows_past_32_bit_byte_offsets():
     ref = ref + x.double()
     ref[6] = ref[5]
     assert bool((torch.abs(got - ref) <= 1e-6 + ref.abs() * (2.0 ** -8 + 2.0 ** -20)).all())
+
+
+def test_outputs_and_gradients_past_32_bit_offsets():
+    # out and dOut of 2^32 + elements; whole numbers whose sums fp32 holds exactly
+    import torch
+    from paper_2605_21442_amd.training import embedding_backward, embedding_forward
+    n, d, v = 530000, 8192, 1000
+    print(f"case n={n} d={d} v={v}", flush=True)
+    w = torch.arange(v, device="cuda:0").remainder(127).to(torch.bfloat16)[:, None].expand(v, d).contiguous()
+    ids = torch.arange(n, device="cuda:0").remainder(v)
+    out, _ = embedding_forward(ids, w)
+    for a in (0, 262143, 524287, 524288, n - 1):
+        assert torch.equal(out[a], w[a % v])
+    assert torch.equal(out[:, 0], w[ids, 0]) and torch.equal(out[:, d - 1], w[ids, 0])
+    x = out
+    x.copy_(torch.arange(n, device="cuda:0").remainder(7).to(torch.bfloat16)[:, None].expand(n, d))
+    dw = embedding_backward(ids, x, v, dw_dtype=torch.float32)
+    ref = torch.zeros(v, dtype=torch.float64, device="cuda:0").index_add_(0, ids, torch.arange(n, device="cuda:0").remainder(7).double())
+    assert bool((dw.double() == ref[:, None]).all())
+
+
+def test_adding_to_a_gradient_is_noticed_by_autograd():
+    import torch
+    from paper_2605_21442_amd.training import embedding_backward
+    a = torch.zeros(4, 8, device="cuda:0")
+    version = a._version
+    embedding_backward(torch.tensor([1, 2], device="cuda:0"), torch.ones(2, 8, device="cuda:0"), 4, accumulate_into=a)
+    assert a._version > version
