@@ -162,8 +162,11 @@ __global__ __launch_bounds__(1024) void k_embed_sort(EmbedRows e, int nb_log2, i
 
 // ---------------------------------------------------------------------------------------------
 // Lookup: a workgroup writes 8192 consecutive elements of out, a thread 8 of every 2048 of them, so that the rows of four
-// pieces are in flight and the stores go in the order of the addresses. They pass the L2 by: kept there, they push out the
-// rows of frequent ids, which are read again and again (32768 tokens of 3584: 82 against 49 us; 16384 of 4096: 42 against 29).
+// pieces are in flight and the stores go in the order of the addresses. kOnce: the stores pass the L2 and the 256 MB MALL by.
+// An output that fits there is better kept, for the layer that reads it next: W cold, 16384 tokens of 4096 (134 MB)
+// looked up and then read take 77 us kept and 88 passed by, 2048 (17 MB) 19 and 22; one that does not fit is better
+// passed by, 32768 (268 MB) 167 and 159. (Lookups of nothing else in a row, whose rows of W then stay in the MALL: 134 MB
+// 37 and 29.5 us, 235 MB 70 and 49.5.)
 // ---------------------------------------------------------------------------------------------
 // 8 elements: as they lie in memory (so that a load is only issued where it stands), and as fp32
 template <typename T> struct Row8;
@@ -210,7 +213,9 @@ struct EmbedIds {
   int64_t n, v_begin, v, padding;
 };
 
-template <typename T>
+constexpr int64_t kKeptBytes = (int64_t)192 << 20;    // of a lookup's output, at most, that is kept
+
+template <typename T, bool kOnce>
 __global__ __launch_bounds__(256) void k_embed_lookup(EmbedIds e, int64_t v_total, const T* __restrict__ W, int64_t ldw,
                                                       int d, float scale, T* __restrict__ out, int* status) {
   constexpr int kAhead = 4;
@@ -246,7 +251,7 @@ __global__ __launch_bounds__(256) void k_embed_lookup(EmbedIds e, int64_t v_tota
       Row8<T>::unpack(raw[k], x);
 #pragma unroll
       for (int c = 0; c < 8; ++c) x[c] = held[k] ? x[c] * scale : 0.f;
-      Row8<T>::template store<true>(out + i[k] * d + col[k], x);
+      Row8<T>::template store<kOnce>(out + i[k] * d + col[k], x);
     }
   }
 }
@@ -475,7 +480,8 @@ template <typename T>
 void launch_lookup(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedIds& e, const void* W, void* out,
                    int32_t* status) {
   const int64_t blocks = (p->n * (p->d / 8) + 1023) / 1024;
-  L(K_EMBED_LOOKUP, k_embed_lookup<T>, dim3((unsigned)std::min<int64_t>(blocks, 1 << 20)), dim3(256), e, pl.v_total,
+  const bool kept = p->n * p->d * (int64_t)sizeof(T) <= kKeptBytes;
+  L(K_EMBED_LOOKUP, kept ? k_embed_lookup<T, false> : k_embed_lookup<T, true>, dim3((unsigned)std::min<int64_t>(blocks, 1 << 20)), dim3(256), e, pl.v_total,
     (const T*)W, pl.ldw, (int)p->d, p->scale, (T*)out, status);
 }
 

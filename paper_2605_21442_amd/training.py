@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import array
 import contextlib
+import itertools
 import math
 import operator
 
@@ -67,7 +68,7 @@ def embedding_forward(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.
     t = _ids(ids, w.device)
     v, d = w.shape
     dev, kind = w.device, _DTYPES[w.dtype]
-    # (B.embedding's structure, in place: a lookup of few tokens is as long as the host takes for it)
+    # (B.embedding's structure, in place: a call of few tokens takes as long as the host does)
     p = B.LceEmbedding(t.numel(), d, v, ldw, 0, v_begin, v_total, B.LCE_NO_PADDING if padding_idx is None else padding_idx,
                        scale, t.element_size(), kind, kind, 0, 0)
     out = torch.empty((*ids.shape, d), dtype=w.dtype, device=dev)
@@ -98,13 +99,14 @@ def embedding_backward(ids: torch.Tensor, grad_out: torch.Tensor, v: int, scale:
         if dw_dtype not in (x.dtype, torch.float32):
             raise TypeError(f"dw_dtype must be {x.dtype} or float32, got {dw_dtype}")
         dw = torch.empty((v, d), dtype=dw_dtype, device=x.device)
-    p = B.embedding(n, d, v, ld_x=ldx, v_begin=v_begin, v_total=v_total, padding_idx=padding_idx, scale=scale,
-                    id_bytes=t.element_size(), dtype=_DTYPES[x.dtype], dw_dtype=_DTYPES[dw.dtype],
-                    flags=B.LCE_FLAG_ACCUMULATE_DW if accumulate_into is not None else 0)
+    dev = x.device
+    p = B.LceEmbedding(n, d, v, 0, ldx, v_begin, v_total, B.LCE_NO_PADDING if padding_idx is None else padding_idx, scale,
+                       t.element_size(), _DTYPES[x.dtype], _DTYPES[dw.dtype],
+                       B.LCE_FLAG_ACCUMULATE_DW if accumulate_into is not None else 0, 0)
     nbytes = B.lce_embedding_workspace_size(p)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
-    with _on(x.device):
-        B.lce_embedding_backward(p, t.data_ptr(), x.data_ptr(), dw.data_ptr(), ws.data_ptr(), nbytes, _stream(x.device))
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    with _on(dev):
+        B.lce_embedding_backward(p, t.data_ptr(), x.data_ptr(), dw.data_ptr(), ws.data_ptr(), nbytes, _stream(dev))
     if accumulate_into is not None and not dw.is_inference():
         increment_version(dw)
     return dw
@@ -291,9 +293,9 @@ class AdamWTensors:
                                        or grad_scale.device != self.device):
             raise ValueError("grad_scale must be a one-element float32 tensor on the parameters' device")
         t = self._table.copy()
-        have = [k for k, g in enumerate(grads) if g is not None]
         shapes = self._shapes
-        if len(have) < len(grads):
+        if any(map(operator.is_, grads, itertools.repeat(None))):
+            have = [k for k, g in enumerate(grads) if g is not None]
             grads, shapes = [grads[k] for k in have], [shapes[k] for k in have]
             t = t[have]                            # (a copy: the tensors without a gradient are not in the call)
         if list(map(_shape_of, grads)) != shapes:
