@@ -9,11 +9,8 @@
 """
 from __future__ import annotations
 
-import array
 import contextlib
-import itertools
 import math
-import operator
 
 import numpy as np
 import torch
@@ -24,6 +21,16 @@ from . import binding as B
 from .autograd import _rows_usable, _stream
 
 _DTYPES = {torch.bfloat16: B.LCE_DTYPE_BF16, torch.float32: B.LCE_DTYPE_F32}
+
+
+def _native():
+    """The extension that reads lists of tensors (csrc/tensors.cpp); like liblce.so it is needed, not replaced."""
+    try:
+        from . import _tensors
+    except ImportError as e:
+        raise RuntimeError("_tensors.so is not built for this Python and torch; run `python -c 'import __graft_entry__ as g; "
+                           "g.build()'` from the repository root") from e
+    return _tensors
 
 
 _HERE = contextlib.nullcontext()
@@ -146,41 +153,34 @@ def token_embedding(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0,
 _GRAD = np.dtype([("data", "u8"), ("n", "i8"), ("dtype", "i4"), ("reserved", "i4")])
 
 
-_dtype_of, _shape_of = operator.attrgetter("dtype"), operator.attrgetter("shape")
-
-
-def _dense(grads: list, dev_index: int | None) -> tuple[list, int | list]:
-    """(the given tensors, contiguous; their lce_dtype_t, one for all where they are alike): what is not contiguous is
-    copied, other types and several devices are refused. A model has hundreds of tensors, so each property is read
-    in one pass over all."""
-    kinds = set(map(_dtype_of, grads))
+def _dense(grads: list, dev_index: int | None) -> tuple[list, list]:
+    """(the given tensors, contiguous; their lce_dtype_t), for lists that the extension does not take as they are: what is
+    not contiguous is copied, other types and several devices are refused."""
+    kinds = {g.dtype for g in grads}
     if not kinds <= _DTYPES.keys():
         raise TypeError(f"gradients must be bfloat16 or float32, got {kinds - _DTYPES.keys()}")
-    where = set(map(torch.Tensor.get_device, grads))
+    where = {g.get_device() for g in grads}
     if -1 in where or len(where) > 1 or (dev_index is not None and where and where != {dev_index}):
         raise ValueError("gradients must be GPU tensors on one device")
-    if not all(map(torch.Tensor.is_contiguous, grads)):
-        grads = [g.contiguous() for g in grads]
-    return grads, [_DTYPES[g.dtype] for g in grads] if len(kinds) > 1 else _DTYPES[kinds.pop()] if kinds else 0
-
-
-def _words(values) -> np.ndarray:
-    """Addresses or counts for a column of a table (numpy takes an array of 64-bit words faster than a list)."""
-    return np.frombuffer(array.array("Q", values), dtype=np.uint64)
+    return [g.resolve_neg().contiguous() for g in grads], [_DTYPES[g.dtype] for g in grads]
 
 
 def grad_norm(grads, max_norm: float = math.inf) -> tuple[torch.Tensor, torch.Tensor]:
     """(norm, factor), fp32 scalars on the device, from lce_grad_norm: the norm of all tensors of ``grads``
     together (None entries are left out) and ``min(1, max_norm / (norm + 1e-6))``, for ``AdamWTensors.step``'s
     ``grad_scale``. The factor is NaN where the norm is not finite. Nothing waits for the device."""
-    grads, dtypes = _dense([g for g in grads if g is not None], None)
-    if not grads:
-        raise ValueError("no gradients")
-    dev = grads[0].device
+    grads = list(grads)
     t = np.zeros(len(grads), dtype=_GRAD)
-    t["data"] = _words(map(torch.Tensor.data_ptr, grads))
-    t["n"] = _words(map(torch.Tensor.numel, grads))
-    t["dtype"] = dtypes
+    first = grads[0].get_device() if grads and grads[0] is not None else -1
+    if first < 0 or not _native().describe(grads, None, first, t, _GRAD.itemsize, 0, 8, 16):
+        grads, dtypes = _dense([g for g in grads if g is not None], None)
+        if not grads:
+            raise ValueError("no gradients")
+        t = np.zeros(len(grads), dtype=_GRAD)
+        t["data"] = [g.data_ptr() for g in grads]
+        t["n"] = [g.numel() for g in grads]
+        t["dtype"] = dtypes
+    dev = grads[0].device
     addr = t.ctypes.data
     nbytes = B.lce_grad_norm_workspace_size(addr, len(grads))
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
@@ -255,7 +255,7 @@ class AdamWTensors:
             self.master = torch.zeros(total, dtype=torch.float32, device=dev)
             for p, o in zip(self.params, self.offsets):
                 self.master[o:o + p.numel()].copy_(p.detach().reshape(-1))
-        self._shapes = [p.shape for p in self.params]
+        self._shapes = [torch.empty(p.shape, device="meta") for p in self.params]
         size = self.exp_avg.element_size()
         t = np.zeros(len(self.params), dtype=_TENSOR)
         off = np.array(self.offsets, dtype=np.uint64)
@@ -270,8 +270,7 @@ class AdamWTensors:
         t["n"] = [p.numel() for p in self.params]
         t["place"], t["group"] = off, at
         t["param_dtype"] = [_DTYPES[p.dtype] for p in self.params]
-        self._table, self._addresses = t, t["param"].tolist()
-        self._tracked = [p for p in self.params if not p.is_inference()]
+        self._table = t
 
     def _seed_of(self, step: int) -> int:
         return (self.seed * 0x9E3779B9 + step * 0x6A09E667) & 0xFFFFFFFF
@@ -284,7 +283,8 @@ class AdamWTensors:
         state's seed and the step. A step captured into a graph keeps the count, the rates and the seed that it
         was captured with in every replay."""
         params = self.params
-        if list(map(torch.Tensor.data_ptr, params)) != self._addresses:
+        native = _native()
+        if not native.stand_at(params, self._table, _TENSOR.itemsize, _TENSOR.fields["param"][1]):
             raise ValueError("a parameter's storage has changed since the state was made")
         grads = [p.grad for p in params] if grads is None else list(grads)
         if len(grads) != len(params):
@@ -293,16 +293,15 @@ class AdamWTensors:
                                        or grad_scale.device != self.device):
             raise ValueError("grad_scale must be a one-element float32 tensor on the parameters' device")
         t = self._table.copy()
-        shapes = self._shapes
-        if any(map(operator.is_, grads, itertools.repeat(None))):
+        if not native.describe(grads, self._shapes, self.device.index, t, _TENSOR.itemsize, _TENSOR.fields["grad"][1], -1,
+                               _TENSOR.fields["grad_dtype"][1]):
             have = [k for k, g in enumerate(grads) if g is not None]
-            grads, shapes = [grads[k] for k in have], [shapes[k] for k in have]
-            t = t[have]                            # (a copy: the tensors without a gradient are not in the call)
-        if list(map(_shape_of, grads)) != shapes:
-            raise ValueError("gradients must be shaped like their parameters")
-        grads, dtypes = _dense(grads, self.device.index)
-        t["grad"] = _words(map(torch.Tensor.data_ptr, grads))
-        t["grad_dtype"] = dtypes
+            grads, t = [grads[k] for k in have], t[have]     # (the tensors without a gradient are not in the call)
+            if any(g.shape != self._shapes[k].shape for g, k in zip(grads, have)):
+                raise ValueError("gradients must be shaped like their parameters")
+            grads, dtypes = _dense(grads, self.device.index)
+            t["grad"] = [g.data_ptr() for g in grads]
+            t["grad_dtype"] = dtypes
         step = self.step_count + 1
         opts = (B.LceAdamW * len(self.groups))(*(
             B.adamw(g["lr"], g["betas"][0], g["betas"][1], g["eps"], g["weight_decay"], step) for g in self.groups))
@@ -310,7 +309,7 @@ class AdamWTensors:
             B.lce_adamw_tensors_step(t.ctypes.data, len(t), opts, len(opts), self.state_bits,
                                      grad_scale.data_ptr() if grad_scale is not None else 0,
                                      self._seed_of(step) if seed is None else seed, _stream(self.device))
-        increment_version(self._tracked)       # a graph that saved a parameter before refuses its backward now
+        native.changed(params)                 # a graph that saved a parameter before refuses its backward now
         self.step_count = step
 
     def moments(self) -> tuple[torch.Tensor, torch.Tensor]:

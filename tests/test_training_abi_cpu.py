@@ -212,3 +212,83 @@ def test_rounding_hash_is_even():
         assert abs(np.corrcoef(x, y)[0, 1]) < 5 / np.sqrt(x.size)
     hist = np.histogram(draws, 64, (0, 1))[0]
     assert np.all(np.abs(hist - draws.size / 64) < 5 * np.sqrt(draws.size / 64))
+
+
+# ---- the extension that reads lists of tensors, on host tensors (device -1) -------------------------
+
+def _native():
+    from paper_2605_21442_amd.training import _native
+    return _native()
+
+
+TABLE = np.dtype([("n", "i8"), ("data", "u8"), ("pad", "i4"), ("dtype", "i4")])
+
+
+def test_describe_fills_a_table():
+    import torch
+    x = torch.zeros(100, dtype=torch.bfloat16)
+    ts = [x, x[3:7], torch.zeros(2, 3), torch.nn.Parameter(torch.zeros(5)), torch.zeros(0)]
+    t = np.full(len(ts), 0, dtype=TABLE)
+    t["pad"] = 77
+    assert _native().describe(ts, None, -1, t, TABLE.itemsize, 8, 0, 20)
+    assert t["data"].tolist() == [a.data_ptr() for a in ts] and t["n"].tolist() == [100, 4, 6, 5, 0]
+    assert t["dtype"].tolist() == [0, 0, 1, 1, 1] and (t["pad"] == 77).all()
+    t["n"] = -5
+    assert _native().describe(ts, [torch.empty(a.shape, device="meta") for a in ts], -1, t, TABLE.itemsize, 8, -1, 20)
+    assert (t["n"] == -5).all()                        # not asked for
+    assert _native().stand_at(ts, t, TABLE.itemsize, 8) and not _native().stand_at(ts[1:], t, TABLE.itemsize, 8)
+    assert _native().describe([], None, -1, t, TABLE.itemsize, 8, 0, 20)
+
+
+def test_describe_leaves_to_the_caller_what_is_not_plain_memory():
+    import torch
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    with FakeTensorMode():
+        fake = torch.empty(4)
+    good = torch.zeros(4, 4)
+    t = np.zeros(2, dtype=TABLE)
+    bad = [None, 3, good.T, good[:, 1:], good.half(), good.to(torch.int32), good.to_sparse(), good.to("meta"), fake]
+    for x in bad:
+        assert not _native().describe([good, x], None, -1, t, TABLE.itemsize, 8, 0, 20), type(x)
+    assert not _native().describe([good], None, 0, t, TABLE.itemsize, 8, 0, 20)          # not on that device
+    assert not _native().describe([good], [torch.zeros(16)], -1, t, TABLE.itemsize, 8, 0, 20)   # another shape
+    assert not _native().describe([good], [None], -1, t, TABLE.itemsize, 8, 0, 20)
+
+
+def test_describe_refuses_a_table_that_does_not_fit():
+    import torch
+    g = torch.zeros(4)
+    t = np.zeros(2, dtype=TABLE)
+    d = _native().describe
+    for args in [([g] * 3, None, -1, t, TABLE.itemsize, 8, 0, 20), ([g], None, -1, t, TABLE.itemsize, 20, 0, 20),
+                 ([g], None, -1, t, TABLE.itemsize, -1, 0, 20), ([g], None, -1, t, TABLE.itemsize, 8, 0, 21),
+                 ([g], None, -1, t, TABLE.itemsize, 8, 20, 20), ([g], None, -1, t, 0, 8, 0, 20), ([g], [g, g], -1, t, TABLE.itemsize, 8, 0, 20)]:
+        with pytest.raises(ValueError):
+            d(*args)
+    with pytest.raises(TypeError):
+        d((g,), None, -1, t, TABLE.itemsize, 8, 0, 20)
+    frozen = np.zeros(2, dtype=TABLE)
+    frozen.flags.writeable = False
+    with pytest.raises(TypeError):                     # the interpreter asks for a writable buffer
+        d([g], None, -1, frozen, TABLE.itemsize, 8, 0, 20)
+    with pytest.raises(TypeError):
+        _native().changed((g,))
+
+
+def test_changed_counts_as_an_in_place_change():
+    import torch
+    p = torch.zeros(3, requires_grad=True)
+    with torch.inference_mode():
+        q = torch.zeros(3)
+    before = p._version
+    _native().changed([p, q, None])
+    assert p._version == before + 1
+
+
+def test_missing_extension_fails_loudly(monkeypatch):
+    import sys
+    from paper_2605_21442_amd import training
+    monkeypatch.setitem(sys.modules, "paper_2605_21442_amd._tensors", None)
+    monkeypatch.delattr("paper_2605_21442_amd._tensors", raising=False)
+    with pytest.raises(RuntimeError, match="not built"):
+        training._native()
