@@ -35,7 +35,7 @@ struct AdamWTable {
   AdamWEntry e[kTableTensors];
   AdamWConst g[kTableGroups];
   int count;
-  int per;                 // elements of a workgroup, a multiple of 2048 (whole rounds of either form)
+  int per;                 // elements of a workgroup, whole rounds
 };
 static_assert(sizeof(AdamWTable) <= 4000, "launch arguments");
 
@@ -470,10 +470,10 @@ lce_status_t lce_adamw_tensors_step(const lce_adamw_tensor_t* tensors, int64_t c
   }
   Launcher L{(hipStream_t)stream};
   AdamWTable t;
-  // elements of a workgroup: 2048, for enough workgroups to fill the card, or up to 8192 where there are more than
-  // 4096 of them, each of which first finds its tensor
-  t.per = 2048;
-  while (t.per < 8192 && total > (int64_t)4096 * t.per) t.per *= 2;
+  // elements of a workgroup: one round (1024 or 2048), for enough workgroups to fill the card, or up to 8192 where there are
+  // more than 8192 of them, each of which first finds its tensor
+  t.per = state_bits == 8 ? 2048 : 1024;
+  while (t.per < 8192 && total > (int64_t)8192 * t.per) t.per *= 2;
   int32_t group_of[kTableGroups];
   int n_table_groups = 0;
   int64_t blocks = 0;
