@@ -13,6 +13,7 @@ TENSORS_SRC = os.path.join(PKG, "csrc", "tensors.cpp")
 TENSORS_OUT = os.path.join(PKG, "_tensors.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CXX = os.environ.get("CXX", "g++")
+ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -43,7 +44,8 @@ def build_tensors(verbose: bool = False) -> str:
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     include = [f"-I{p}" for p in (*cpp_extension.include_paths(), sysconfig.get_paths()["include"])]
     _run([CXX, "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
-          *include, TENSORS_SRC, f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10"], TENSORS_OUT, verbose)
+          "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", *include, f"-I{os.path.join(ROCM, 'include')}", TENSORS_SRC,
+          f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"], TENSORS_OUT, verbose)
     return TENSORS_OUT
 
 

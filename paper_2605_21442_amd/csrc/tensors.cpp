@@ -7,6 +7,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/hip/HIPStream.h>
 
 #include <cstdint>
 #include <cstring>
@@ -114,9 +115,23 @@ PyObject* changed(PyObject*, PyObject* list) {
   Py_RETURN_NONE;
 }
 
+// current_stream(device) -> int: the hipStream_t that torch works on there (0: the default stream). Through torch's Stream
+// object this takes 2 us, a sixth of a small call.
+PyObject* current_stream(PyObject*, PyObject* device) {
+  const long index = PyLong_AsLong(device);
+  if (index == -1 && PyErr_Occurred()) return nullptr;
+  try {
+    return PyLong_FromVoidPtr(c10::hip::getCurrentHIPStream(static_cast<c10::DeviceIndex>(index)).stream());
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
 PyMethodDef methods[] = {{"describe", describe, METH_VARARGS, nullptr},
                          {"stand_at", stand_at, METH_VARARGS, nullptr},
                          {"changed", changed, METH_O, nullptr},
+                         {"current_stream", current_stream, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -18,19 +18,29 @@ from torch.autograd.function import once_differentiable
 from torch.autograd.graph import increment_version
 
 from . import binding as B
-from .autograd import _rows_usable, _stream
+from .autograd import _rows_usable
 
 _DTYPES = {torch.bfloat16: B.LCE_DTYPE_BF16, torch.float32: B.LCE_DTYPE_F32}
 
 
+_ext = None
+
+
 def _native():
     """The extension that reads lists of tensors (csrc/tensors.cpp); like liblce.so it is needed, not replaced."""
-    try:
-        from . import _tensors
-    except ImportError as e:
-        raise RuntimeError("_tensors.so is not built for this Python and torch; run `python -c 'import __graft_entry__ as g; "
-                           "g.build()'` from the repository root") from e
-    return _tensors
+    global _ext
+    if _ext is None:
+        try:
+            from . import _tensors
+        except ImportError as e:
+            raise RuntimeError("_tensors.so is not built for this Python and torch; run `python -c 'import __graft_entry__ as "
+                               "g; g.build()'` from the repository root") from e
+        _ext = _tensors
+    return _ext
+
+
+def _stream(dev: torch.device) -> int:
+    return _native().current_stream(dev.index)
 
 
 _HERE = contextlib.nullcontext()

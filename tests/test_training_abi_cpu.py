@@ -288,6 +288,7 @@ def test_changed_counts_as_an_in_place_change():
 def test_missing_extension_fails_loudly(monkeypatch):
     import sys
     from paper_2605_21442_amd import training
+    monkeypatch.setattr(training, "_ext", None)
     monkeypatch.setitem(sys.modules, "paper_2605_21442_amd._tensors", None)
     monkeypatch.delattr("paper_2605_21442_amd._tensors", raising=False)
     with pytest.raises(RuntimeError, match="not built"):
