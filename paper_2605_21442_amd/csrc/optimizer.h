@@ -311,12 +311,13 @@ __global__ __launch_bounds__(256) void k_adamw_moments(int64_t n, const uint8_t*
 // workgroup adds these in order. fp64: an fp32 square overflows from 1.8e19 on, which bf16 holds, and a
 // model's 1e9 squares lose digits in fp32.
 // ---------------------------------------------------------------------------------------------
-struct NormEntry {
+struct NormEntry {        // of a tensor, or of 2^30 elements of a larger one
   const void* data;
-  int64_t n;
-  uint32_t first, f32;
+  uint32_t n;
+  uint32_t first : 31, f32 : 1;
 };
-constexpr int kNormTensors = 160;
+constexpr int64_t kNormEntryElems = (int64_t)1 << 30;
+constexpr int kNormTensors = 248;
 struct NormTable {
   NormEntry e[kNormTensors];
   int count;
@@ -357,8 +358,8 @@ __global__ __launch_bounds__(256) void k_grad_squares(NormTable t, int64_t bytes
   constexpr int kAhead = 8;
   const NormEntry e = t.e[table_entry(t.e, t.count, blockIdx.x)];
   const int size = e.f32 ? 4 : 2;
-  const int64_t head = min(e.n, (int64_t)((16 - ((uintptr_t)e.data & 15)) & 15) / size);
-  const int64_t pieces = (e.n - head) * size / 16;
+  const int64_t n = e.n, head = min(n, (int64_t)((16 - ((uintptr_t)e.data & 15)) & 15) / size);
+  const int64_t pieces = (n - head) * size / 16;
   const uint4* p = reinterpret_cast<const uint4*>((const char*)e.data + head * size);
   const int64_t q0 = (int64_t)(blockIdx.x - e.first) * (bytes / 16), q1 = min(pieces, q0 + bytes / 16);
   double sum = 0;
@@ -372,7 +373,7 @@ __global__ __launch_bounds__(256) void k_grad_squares(NormTable t, int64_t bytes
   if (blockIdx.x == e.first) {
     const int64_t tail = head + pieces * 16 / size;
     const int64_t i = threadIdx.x < 8 ? threadIdx.x : tail + threadIdx.x - 8;     // at most 7 on either side
-    if (threadIdx.x < 8 ? i < head : threadIdx.x < 16 && i < e.n) {
+    if (threadIdx.x < 8 ? i < head : threadIdx.x < 16 && i < n) {
       const double x = e.f32 ? ((const float*)e.data)[i] : bf16_to_f32(((const uint16_t*)e.data)[i]);
       sum += x * x;
     }
@@ -421,8 +422,18 @@ lce_status_t check_adamw_tensor(const lce_adamw_tensor_t& t, int32_t n_groups, i
   return LCE_OK;
 }
 
-inline int64_t norm_blocks(const lce_grad_t& g, int64_t bytes) {
+inline int64_t norm_part_blocks(const lce_grad_t& g, int64_t bytes) {
   return (g.n * (int64_t)dtype_bytes(g.dtype) + bytes - 1) / bytes;
+}
+
+inline int64_t norm_blocks(lce_grad_t g, int64_t bytes) {
+  int64_t blocks = 0;
+  for (; g.n > kNormEntryElems; g.n -= kNormEntryElems) {
+    lce_grad_t part = g;
+    part.n = kNormEntryElems;
+    blocks += norm_part_blocks(part, bytes);
+  }
+  return blocks + norm_part_blocks(g, bytes);
 }
 
 // *bytes: what a workgroup of k_grad_squares takes, 32 KB (one round of loads) or as many times that as keep the
@@ -556,11 +567,13 @@ lce_status_t lce_grad_norm(const lce_grad_t* grads, int64_t count, float max_nor
   };
   for (int64_t i = 0; i < count; ++i) {
     const lce_grad_t& g = grads[i];
-    if (g.n == 0) continue;
-    const int64_t nb = norm_blocks(g, bytes);
-    if (t.count == kNormTensors || here + nb > kMostBlocks) flush();
-    t.e[t.count++] = NormEntry{g.data, g.n, (uint32_t)here, (uint32_t)(g.dtype == LCE_DTYPE_F32)};
-    here += nb;
+    for (int64_t at = 0; at < g.n; at += kNormEntryElems) {
+      const lce_grad_t part{(const char*)g.data + at * dtype_bytes(g.dtype), std::min(g.n - at, kNormEntryElems), g.dtype, 0};
+      const int64_t nb = norm_part_blocks(part, bytes);
+      if (t.count == kNormTensors || here + nb > kMostBlocks) flush();
+      t.e[t.count++] = NormEntry{part.data, (uint32_t)part.n, (uint32_t)here, (uint32_t)(g.dtype == LCE_DTYPE_F32)};
+      here += nb;
+    }
   }
   flush();
   L(K_GRAD_NORM, k_grad_norm, dim3(1), dim3(1024), (const double*)parts, blocks, max_norm, norm, factor);
