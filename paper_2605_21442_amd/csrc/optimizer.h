@@ -1,5 +1,5 @@
 // AdamW over many tensors (moments in 32 or 8 bits) and the norm of many gradients. Included by lce.hip,
-// behind its launcher. A launch serves up to kTableTensors tensors, whose addresses travel in its arguments: nothing
+// behind its launcher. A launch serves dozens of tensors, whose addresses travel in its arguments: nothing
 // is copied to the device beforehand, so a call can be captured and its table needs no storage.
 //
 // All of it is bound by memory on a whole model (1.2e9 bf16 elements): the 32-bit step with an fp32 master copy moves
@@ -13,31 +13,38 @@ namespace {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kTableTensors = 48;
 constexpr int kTableGroups = 8;
 constexpr int kMomentBlock = 32;       // elements that share the units of the 8-bit moments
+constexpr int64_t kEntryElems = (int64_t)1 << 30;      // a larger tensor takes several entries
 
-struct AdamWEntry {
+template <int kBits> struct AdamWEntry;
+template <> struct AdamWEntry<32> {
   void* param;
   const void* grad;
   void* m;
   void* v;
-  uint8_t* units;
   float* master;
-  int64_t n;
-  uint32_t first;          // first workgroup of this tensor
+  uint32_t n;
+  uint32_t first : 24;     // first workgroup of this entry
+  uint32_t group : 3, param_f32 : 1, grad_f32 : 1;
+  uint32_t wide : 3;       // bits: param, grad, master lie at a multiple of 16 bytes
+};
+template <> struct AdamWEntry<8> : AdamWEntry<32> {
+  uint8_t* units;
   uint32_t pair0;          // place / 2
-  uint8_t group, param_f32, grad_f32;
-  uint8_t wide;            // bits: param, grad, master lie at a multiple of 16 bytes
+  uint32_t pad_;
 };
 
+// 77 tensors a launch with 32-bit moments, 58 with 8-bit ones, and the groups' constants
+template <int kBits>
 struct AdamWTable {
-  AdamWEntry e[kTableTensors];
+  static constexpr int kTensors = kBits == 32 ? 77 : 58;
+  AdamWEntry<kBits> e[kTensors];
   AdamWConst g[kTableGroups];
   int count;
   int per;                 // elements of a workgroup, whole rounds
 };
-static_assert(sizeof(AdamWTable) <= 4000, "launch arguments");
+static_assert(sizeof(AdamWTable<32>) <= 4000 && sizeof(AdamWTable<8>) <= 4000, "launch arguments");
 
 // The entry of workgroup `block`: the last one whose first workgroup is not behind it, found by all lanes at once.
 template <typename Entry>
@@ -178,7 +185,7 @@ __device__ __forceinline__ float adamw_update_near(float& p, float& m, float r, 
 }
 
 // 32-bit moments: 4 elements per thread and round, so that every access of a wave is contiguous.
-__device__ __forceinline__ void adamw_round32(const AdamWEntry& e, const AdamWConst& c, int64_t i, float scale, bool scaled) {
+__device__ __forceinline__ void adamw_round32(const AdamWEntry<32>& e, const AdamWConst& c, int64_t i, float scale, bool scaled) {
 #pragma clang fp contract(off)
   float p[4], g[4] = {}, m[4], v[4];
   load_elems<4>(e.m, i, e.n, true, true, m);
@@ -199,7 +206,7 @@ __device__ __forceinline__ void adamw_round32(const AdamWEntry& e, const AdamWCo
 
 // 8-bit moments: 8 elements per thread and round, four lanes to a block. Every lane of a wave comes here (the
 // blocks' maxima pass between lanes); those at or past n hold zeros.
-__device__ __forceinline__ void adamw_round8(const AdamWEntry& e, const AdamWConst& c, int64_t i, float scale, bool scaled,
+__device__ __forceinline__ void adamw_round8(const AdamWEntry<8>& e, const AdamWConst& c, int64_t i, float scale, bool scaled,
                                              uint32_t seed) {
 #pragma clang fp contract(off)
   float p[8] = {}, g[8] = {}, m[8] = {}, r[8] = {};
@@ -266,10 +273,10 @@ __device__ __forceinline__ void adamw_round8(const AdamWEntry& e, const AdamWCon
 }
 
 template <int kBits>
-__global__ __launch_bounds__(256) void k_adamw_tensors(AdamWTable t, const float* __restrict__ grad_scale, uint32_t seed) {
+__global__ __launch_bounds__(256) void k_adamw_tensors(AdamWTable<kBits> t, const float* __restrict__ grad_scale, uint32_t seed) {
   const float scale = grad_scale ? *grad_scale : 1.0f;
   if (!(fabsf(scale) < INFINITY)) return;
-  const AdamWEntry e = t.e[table_entry(t.e, t.count, blockIdx.x)];
+  const AdamWEntry<kBits> e = t.e[table_entry(t.e, t.count, blockIdx.x)];
   const AdamWConst c = t.g[e.group];
   constexpr int kPer = kBits == 32 ? 4 : 8;
   const int64_t i0 = (int64_t)(blockIdx.x - e.first) * t.per;
@@ -459,6 +466,68 @@ lce_status_t check_grads(const lce_grad_t* grads, int64_t count, int64_t* bytes,
   return LCE_OK;
 }
 
+// the entry of elements [at, at + n) of a tensor
+void fill_entry(AdamWEntry<32>* e, const lce_adamw_tensor_t& x, int64_t at, int64_t n, int64_t first, int group, int bits) {
+  const auto off = [at](const void* p, int64_t size) { return p ? (char*)p + at * size : nullptr; };
+  e->param = off(x.param, dtype_bytes(x.param_dtype));
+  e->grad = off(x.grad, dtype_bytes(x.grad_dtype));
+  e->m = off(x.exp_avg, bits / 8);
+  e->v = off(x.exp_avg_sq, bits / 8);
+  e->master = (float*)off(x.master, 4);
+  e->n = (uint32_t)n;
+  e->first = (uint32_t)first;
+  e->group = (uint32_t)group;
+  e->param_f32 = x.param_dtype == LCE_DTYPE_F32;
+  e->grad_f32 = x.grad_dtype == LCE_DTYPE_F32;
+  e->wide = aligned16(x.param) | aligned16(x.grad) << 1 | aligned16(x.master) << 2;
+}
+
+void fill_entry(AdamWEntry<8>* e, const lce_adamw_tensor_t& x, int64_t at, int64_t n, int64_t first, int group, int bits) {
+  fill_entry(static_cast<AdamWEntry<32>*>(e), x, at, n, first, group, bits);
+  e->units = (uint8_t*)x.units + at / 16;
+  e->pair0 = (uint32_t)((uint64_t)(x.place + at) >> 1);
+  e->pad_ = 0;
+}
+
+template <int kBits>
+void launch_adamw(Launcher& L, const lce_adamw_tensor_t* tensors, int64_t count, const lce_adamw_t* groups, int64_t total,
+                  const float* grad_scale, uint32_t seed) {
+  AdamWTable<kBits> t;
+  // elements of a workgroup: one round (1024 or 2048), for enough workgroups to fill the card, or up to 8192 where there are
+  // more than 8192 of them, each of which first finds its tensor
+  t.per = kBits == 8 ? 2048 : 1024;
+  while (t.per < 8192 && total > (int64_t)8192 * t.per) t.per *= 2;
+  int32_t group_of[kTableGroups];
+  int n_groups = 0;
+  int64_t blocks = 0;
+  t.count = 0;
+  const auto flush = [&] {
+    if (t.count == 0) return;
+    L(K_ADAMW_TENSORS, k_adamw_tensors<kBits>, dim3((unsigned)blocks), dim3(256), t, grad_scale, seed);
+    t.count = n_groups = 0;
+    blocks = 0;
+  };
+  for (int64_t i = 0; i < count; ++i) {
+    const lce_adamw_tensor_t& x = tensors[i];
+    for (int64_t at = 0; at < x.n; at += kEntryElems) {
+      const int64_t n = std::min(x.n - at, kEntryElems), nb = (n + t.per - 1) / t.per;
+      int g = 0;
+      while (g < n_groups && group_of[g] != x.group) ++g;
+      if (t.count == AdamWTable<kBits>::kTensors || g == kTableGroups || blocks + nb > kMostBlocks) {
+        flush();
+        g = 0;
+      }
+      if (g == n_groups) {
+        (void)make_adamw(&groups[x.group], &t.g[g]);
+        group_of[n_groups++] = x.group;
+      }
+      fill_entry(&t.e[t.count++], x, at, n, blocks, g, kBits);
+      blocks += nb;
+    }
+  }
+  flush();
+}
+
 }  // namespace
 
 extern "C" {
@@ -480,43 +549,8 @@ lce_status_t lce_adamw_tensors_step(const lce_adamw_tensor_t* tensors, int64_t c
     total += tensors[i].n;
   }
   Launcher L{(hipStream_t)stream};
-  AdamWTable t;
-  // elements of a workgroup: one round (1024 or 2048), for enough workgroups to fill the card, or up to 8192 where there are
-  // more than 8192 of them, each of which first finds its tensor
-  t.per = state_bits == 8 ? 2048 : 1024;
-  while (t.per < 8192 && total > (int64_t)8192 * t.per) t.per *= 2;
-  int32_t group_of[kTableGroups];
-  int n_table_groups = 0;
-  int64_t blocks = 0;
-  t.count = 0;
-  const auto flush = [&] {
-    if (t.count == 0) return;
-    const auto kernel = state_bits == 8 ? k_adamw_tensors<8> : k_adamw_tensors<32>;
-    L(K_ADAMW_TENSORS, kernel, dim3((unsigned)blocks), dim3(256), t, grad_scale, seed);
-    t.count = n_table_groups = 0;
-    blocks = 0;
-  };
-  for (int64_t i = 0; i < count; ++i) {
-    const lce_adamw_tensor_t& x = tensors[i];
-    if (x.n == 0) continue;
-    const int64_t nb = (x.n + t.per - 1) / t.per;
-    int g = 0;
-    while (g < n_table_groups && group_of[g] != x.group) ++g;
-    if (t.count == kTableTensors || g == kTableGroups || blocks + nb > kMostBlocks) {
-      flush();
-      g = 0;
-    }
-    if (g == n_table_groups) {
-      (void)make_adamw(&groups[x.group], &t.g[g]);
-      group_of[n_table_groups++] = x.group;
-    }
-    t.e[t.count++] = AdamWEntry{x.param, x.grad, x.exp_avg, x.exp_avg_sq, (uint8_t*)x.units, x.master, x.n,
-                                (uint32_t)blocks, (uint32_t)((uint64_t)x.place >> 1), (uint8_t)g,
-                                (uint8_t)(x.param_dtype == LCE_DTYPE_F32), (uint8_t)(x.grad_dtype == LCE_DTYPE_F32),
-                                (uint8_t)(aligned16(x.param) | aligned16(x.grad) << 1 | aligned16(x.master) << 2)};
-    blocks += nb;
-  }
-  flush();
+  if (state_bits == 8) launch_adamw<8>(L, tensors, count, groups, total, grad_scale, seed);
+  else launch_adamw<32>(L, tensors, count, groups, total, grad_scale, seed);
   return L.st;
 }
 
