@@ -425,6 +425,92 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedSorted s, int v, int d,
 }
 
 // ---------------------------------------------------------------------------------------------
+// Gradient of few tokens, without a sort: a workgroup per token and 512 columns lists the tokens of its token's id, in order,
+// from a look at all ids, and goes on if its own is the first of them. Its four waves add a quarter of the rows each, eight
+// in flight, and the quarters are added in order. A fresh dW is zeroed by a launch before.
+// Two launches (one where dW is added to) instead of three, whose latencies are all that few tokens cost.
+// ---------------------------------------------------------------------------------------------
+constexpr int kFewTokens = 1024;
+
+template <typename T, typename TW, bool kAdd, int kBytes>
+__global__ __launch_bounds__(256) void k_embed_few(EmbedRows e, const T* __restrict__ dout, int64_t ldx, int d, int slices,
+                                                   float scale, TW* __restrict__ dw) {
+  constexpr int kAhead = 8, kGroups = kFewTokens / 256;      // groups of 64 ids per wave
+  typedef typename std::conditional<kBytes == 8, uint64_t, uint32_t>::type Id;
+  __shared__ int list[kFewTokens], found[4], earlier[4];
+  __shared__ float sums[3][kGradCols];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = (int)e.n;
+  const int token = blockIdx.x / slices;
+  const int col0 = (blockIdx.x - token * slices) * kGradCols + lane * 8;
+  const bool live = col0 < d;
+  const int col = live ? col0 : 0;             // (lanes behind the row read its start and store nothing)
+  const Id* ids = (const Id*)e.ids;
+  Id id[kGroups];
+#pragma unroll
+  for (int k = 0; k < kGroups; ++k) id[k] = ids[min(w * (64 * kGroups) + 64 * k + lane, n - 1)];
+  const Id mine = ids[token];
+  const Id r = mine - (Id)e.v_begin;
+  if (r >= e.v || (int)r == e.pad_row) return;
+  TW* o = dw + (int64_t)r * d + col;
+  typename Row8<TW>::Raw old{};
+  if (kAdd) old = Row8<TW>::fetch(o);
+  unsigned long long same[kGroups];
+  int count = 0;
+  bool before = false;
+#pragma unroll
+  for (int k = 0; k < kGroups; ++k) {
+    const int t = w * (64 * kGroups) + 64 * k + lane;
+    same[k] = __ballot(t < n && id[k] == mine);
+    before |= __ballot(t < token && id[k] == mine) != 0;
+    count += __popcll(same[k]);
+  }
+  if (lane == 0) {
+    found[w] = count;
+    earlier[w] = before;
+  }
+  __syncthreads();
+  if (earlier[0] | earlier[1] | earlier[2] | earlier[3]) return;      // another workgroup's id
+  int at = 0;
+  for (int k = 0; k < w; ++k) at += found[k];
+#pragma unroll
+  for (int k = 0; k < kGroups; ++k) {
+    if ((same[k] >> lane) & 1) list[at + __popcll(same[k] & ((1ull << lane) - 1ull))] = w * (64 * kGroups) + 64 * k + lane;
+    at += __popcll(same[k]);
+  }
+  __syncthreads();
+  const int total = found[0] + found[1] + found[2] + found[3], quarter = (total + 3) / 4;
+  const int p1 = min(total, (w + 1) * quarter);
+  float sum[8] = {};
+  for (int p = w * quarter; p < p1; p += kAhead) {
+    typename Row8<T>::Raw x[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) x[k] = Row8<T>::fetch(dout + (int64_t)list[min(p + k, p1 - 1)] * ldx + col);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      float y[8];
+      Row8<T>::unpack(x[k], y);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) sum[c] += p + k < p1 ? y[c] : 0.f;
+    }
+  }
+  if (w > 0)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) sums[w - 1][c * 64 + lane] = sum[c];
+  __syncthreads();
+  if (w > 0 || !live) return;
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) sum[c] += sums[k][c * 64 + lane];
+  grad_store<TW, kAdd>(o, old, sum, scale);
+}
+
+__global__ __launch_bounds__(256) void k_embed_zero(char* __restrict__ dw, int64_t bytes) {
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 16;
+  if (at < bytes) store16_padded(dw + at, i32x4_t{0, 0, 0, 0});
+}
+
+// ---------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------
 struct EmbedPlan {
@@ -496,6 +582,25 @@ void launch_embed_grad(Launcher& L, const lce_embedding_t* p, const EmbedPlan& p
     pl.slices, join, p->scale, (TW*)dw, (const float*)parts);
 }
 
+// Up to 1024 tokens, and 4096 workgroups.
+inline bool few_tokens(const lce_embedding_t* p, const EmbedPlan& pl) {
+  return p->n <= kFewTokens && p->n * pl.slices <= 4096;
+}
+
+template <typename T, typename TW, bool kAdd>
+void launch_embed_few(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedRows& e, const void* dout, void* dw) {
+  const int64_t bytes = p->v * p->d * (int64_t)sizeof(TW);
+  if (!kAdd) L(K_EMBED_GRAD, k_embed_zero, dim3((unsigned)((bytes + 4095) / 4096)), dim3(256), (char*)dw, bytes);
+  L(K_EMBED_GRAD, p->id_bytes == 8 ? k_embed_few<T, TW, kAdd, 8> : k_embed_few<T, TW, kAdd, 4>,
+    dim3((unsigned)(p->n * pl.slices)), dim3(256), e, (const T*)dout, pl.ldx, (int)p->d, pl.slices, p->scale, (TW*)dw);
+}
+
+template <typename T, typename TW>
+void launch_embed_few(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedRows& e, const void* dout, void* dw) {
+  if (p->flags & LCE_FLAG_ACCUMULATE_DW) launch_embed_few<T, TW, true>(L, p, pl, e, dout, dw);
+  else launch_embed_few<T, TW, false>(L, p, pl, e, dout, dw);
+}
+
 template <typename T, typename TW>
 void launch_embed_grad(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedSorted& s, const void* dout,
                        void* dw, float* parts) {
@@ -545,6 +650,12 @@ lce_status_t lce_embedding_backward(const lce_embedding_t* p, const void* ids, c
   int* starts = (int*)(ws + pl.o_starts);
   const bool pad = p->padding_idx >= p->v_begin && p->padding_idx < p->v_begin + p->v;
   const EmbedRows e{ids, p->n, p->v_begin, (uint32_t)p->v, pad ? (int)(p->padding_idx - p->v_begin) : -1};
+  if (few_tokens(p, pl)) {
+    if (p->dtype == LCE_DTYPE_F32) launch_embed_few<float, float>(L, p, pl, e, dOut, dW);
+    else if (p->dw_dtype == LCE_DTYPE_F32) launch_embed_few<uint16_t, float>(L, p, pl, e, dOut, dW);
+    else launch_embed_few<uint16_t, uint16_t>(L, p, pl, e, dOut, dW);
+    return L.st;
+  }
   L(K_EMBED_SORT, p->id_bytes == 8 ? k_embed_sort<8> : k_embed_sort<4>, dim3(1u << pl.nb_log2), dim3(64 * kSortWaves), e,
     pl.nb_log2, pl.rows, sorted, starts);
   const EmbedSorted s{sorted, starts, pl.nb_log2, pl.rows};
