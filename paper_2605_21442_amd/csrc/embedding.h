@@ -574,8 +574,10 @@ void launch_lookup(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, c
 template <typename T, typename TW, bool kAdd>
 void launch_embed_grad(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedSorted& s, const void* dout,
                        void* dw, float* parts) {
-  const int64_t units = pl.chunks * pl.slices, join = pl.chunks > 1 ? units : 0;
-  const int64_t fill = kAdd ? 0 : (p->v * p->d * (int64_t)sizeof(TW) + kFillBytes - 1) / kFillBytes;
+  const int64_t units = pl.chunks * pl.slices, join = pl.chunks > 1 ? units : 0, bytes = p->v * p->d * (int64_t)sizeof(TW);
+  const bool zero = !kAdd && p->n <= p->v / 4;
+  const int64_t fill = kAdd || zero ? 0 : (bytes + kFillBytes - 1) / kFillBytes;
+  if (zero) L(K_EMBED_GRAD, k_embed_zero, dim3((unsigned)((bytes + 4095) / 4096)), dim3(256), (char*)dw, bytes);
   L(K_EMBED_GRAD, k_embed_grad<T, TW, kAdd>, dim3((unsigned)((units + 3) / 4)), dim3(256), s, (const T*)dout, pl.ldx,
     (int)p->d, pl.per, units, pl.slices, p->scale, (TW*)dw, parts);
   L(K_EMBED_GRAD, k_embed_join<TW, kAdd>, dim3((unsigned)(join + fill)), dim3(256), s, (int)p->v, (int)p->d, pl.per,
