@@ -2,8 +2,9 @@
 //
 // The gradient adds each id's tokens in an order that the ids alone fix, without atomics on sums:
 //   sort: tokens grouped by id, in token order within an id (a stable counting sort, one launch);
-//   grad: the fp32 sums of the rows of dOut by runs of sorted tokens, and the rows without tokens;
-//   join: the sums of the ids that several runs share.
+//   grad: the fp32 sums of the rows of dOut by runs of sorted tokens;
+//   join: the sums of the ids that several runs share; and, in a fresh dW, the rows without tokens (or a launch before).
+// Few tokens take one launch for all of it (k_embed_few).
 #pragma once
 
 namespace {
@@ -18,7 +19,7 @@ namespace {
 // bucket in LDS as it counts them, so only one with more than the list holds walks the ids twice.
 // 709 / 4096 / 16384 / 65070 tokens: 6.2 / 7.2 / 10.2 / 30 us. Short batches are bound by the chain of loads, barriers and the
 // scan; long ones by the vector instructions of the walk (every bucket looks at every id) in the bucket of the
-// most frequent id, half a microsecond per 1000 tokens. (Ranks by one ballot per bit for every group of 64 tokens, without
+// most frequent id, 0.3 to 0.5 us per 1000 tokens. (Ranks by one ballot per bit for every group of 64 tokens, without
 // the lists: 22 us for 16384 tokens; ids loaded one group at a time: 30.)
 // ---------------------------------------------------------------------------------------------
 constexpr int kSortWaves = 16;
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(256) void k_embed_grad(EmbedSorted s, const T* __re
 }
 
 // The rows of a fresh dW without a token, in the order of the addresses: 16 KB of dW per workgroup, 16 bytes of each
-// 4 KB per thread. (128256 x 4096 bf16 in pieces of 16 KB: 6.7 TB/s, as a fill without a look at the rows; of 4 KB, whose
+// 4 KB per thread. (All rows of 128256 x 4096 bf16 in pieces of 16 KB: 6.7 TB/s, as a fill without a look at the rows; of 4 KB, whose
 // two loads come before the one store, 5.1; whole rows by wave 5.5 to 6.0.)
 constexpr int kFillAhead = 4;
 constexpr int64_t kFillBytes = 256 * 16 * kFillAhead;
@@ -428,7 +429,10 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedSorted s, int v, int d,
 // Gradient of few tokens, without a sort: a workgroup per token and 512 columns lists the tokens of its token's id, in order,
 // from a look at all ids, and goes on if its own is the first of them. Its four waves add a quarter of the rows each, eight
 // in flight, and the quarters are added in order. A fresh dW is zeroed by a launch before.
-// Two launches (one where dW is added to) instead of three, whose latencies are all that few tokens cost.
+// Two launches (one where dW is added to) instead of three, whose latencies are all that few tokens cost. Added, replayed:
+// 256 tokens of 512 columns 3.9 us against 13.0 by the sort, 1024 of 2048 9.4 against 14.8; 4096 workgroups are the
+// limit (1024 of 4096 26 against 16) and 1024 tokens too, for the batch whose tokens are all one id (1024 of 512 23.5 against
+// 15.5, 2048 45 against 19).
 // ---------------------------------------------------------------------------------------------
 constexpr int kFewTokens = 1024;
 
@@ -538,8 +542,8 @@ lce_status_t make_embed_plan(const lce_embedding_t* p, EmbedPlan* pl) {
   pl->ldx = p->ld_x ? p->ld_x : p->d;
   if (pl->ldw < p->d || pl->ldx < p->d || pl->ldw >= (int64_t)1 << 30 || pl->ldx >= (int64_t)1 << 30) return LCE_ERR_SHAPE;
   if (pl->ldw % 8 != 0 || pl->ldx % 8 != 0) return LCE_ERR_ALIGN;
-  // a launch takes fewer than 2^32 threads, and zeroes 16 KB of dW with 256 of them
-  if ((uint64_t)p->v * p->d * (p->dw_dtype == LCE_DTYPE_F32 ? 4 : 2) > (uint64_t)1 << 37) return LCE_ERR_SHAPE;
+  // a launch takes fewer than 2^32 threads, and zeroes 4 KB of dW with 256 of them
+  if ((uint64_t)p->v * p->d * (p->dw_dtype == LCE_DTYPE_F32 ? 4 : 2) > (uint64_t)1 << 35) return LCE_ERR_SHAPE;
   // 256 buckets, one per CU, or as many as keep a bucket's counts in LDS; no more than there are ids
   pl->nb_log2 = 0;
   while (pl->nb_log2 < 8 && ((int64_t)1 << pl->nb_log2) < p->v) ++pl->nb_log2;
@@ -575,7 +579,10 @@ template <typename T, typename TW, bool kAdd>
 void launch_embed_grad(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedSorted& s, const void* dout,
                        void* dw, float* parts) {
   const int64_t units = pl.chunks * pl.slices, join = pl.chunks > 1 ? units : 0, bytes = p->v * p->d * (int64_t)sizeof(TW);
-  const bool zero = !kAdd && p->n <= p->v / 4;
+  // a fresh dW is zeroed whole before where few of its rows can have tokens and the launch is short beside it (4096
+  // tokens, 128256 x 2048 / 8192: 102 / 360 us, row by row behind the sums 111 / 397; but 2048 tokens, 128256 x 512:
+  // 35 against 33; 16384, 32000 x 4096: 106 against 103; 65536, 128256 x 4096 of even ids: 406 against 363)
+  const bool zero = !kAdd && p->n <= p->v / 4 && bytes >= (int64_t)256 << 20;
   const int64_t fill = kAdd || zero ? 0 : (bytes + kFillBytes - 1) / kFillBytes;
   if (zero) L(K_EMBED_GRAD, k_embed_zero, dim3((unsigned)((bytes + 4095) / 4096)), dim3(256), (char*)dw, bytes);
   L(K_EMBED_GRAD, k_embed_grad<T, TW, kAdd>, dim3((unsigned)((units + 3) / 4)), dim3(256), s, (const T*)dout, pl.ldx,

@@ -169,8 +169,8 @@ __device__ __forceinline__ void decode_moments(const uint2 cm, const uint2 cr, i
 // AdamW's update of one element as adamw_update has it, but for the root and the quotient: each is the hardware's estimate
 // (1 ulp) with one Newton step, which is the correctly rounded value but for a few in a million. The compiler's own
 // sequences, which are right for every operand, made the 8-bit step bound by the vector units (91 instructions an
-// element, 3.04 ms for 1.2e9). Here v is 0 or at least 2^-126 where |g| > 1e-18; below, the root is only of the
-// order of magnitude. Where v or the quotient overflows, the result is NaN. Returns the root.
+// element, 3.04 ms for 1.2e9). v is 0 or at least 2^-126 where |g| > 1e-17; a smaller one has too small a root, which eps
+// hides. Where v or the quotient overflows, the result is NaN. Returns the root.
 __device__ __forceinline__ float adamw_update_near(float& p, float& m, float r, float g, const AdamWConst& c) {
 #pragma clang fp contract(off)
   p = p * c.keep;

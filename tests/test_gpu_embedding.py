@@ -149,6 +149,33 @@ def test_gradient_of_long_batches(n, d, v):
     assert bool((torch.abs(dw.double() - ref) <= tol + (ref.abs() + tol) * 2.0 ** -8).all())
 
 
+@pytest.mark.parametrize("kind", ["one", "zipf"])
+@pytest.mark.parametrize("n,d,v", [(1024, 2048, 3000), (1024, 2056, 3000), (1025, 512, 3000), (512, 4096, 700), (513, 4096, 700),
+                                   (4, 1 << 16, 9), (900, 8, 1 << 19)])
+def test_gradient_where_its_forms_meet(n, d, v, kind):
+    # with and without the sort, one after the other of either size
+    import torch
+    from paper_2605_21442_amd.training import embedding_backward
+    print(f"case forms n={n} d={d} v={v} {kind}", flush=True)
+    ids, x = _id_list(n, v, 62, kind), _draw((n, d), "bf16", 63)
+    ids[::7] = v + 5
+    t = torch.from_numpy(ids).to("cuda:0")
+    dw = embedding_backward(t, x, v, 0.25, padding_idx=1)
+    ref = torch.zeros(v + 6, d, dtype=torch.float64, device="cuda:0").index_add_(0, t, x.double() * 0.25)[:v]
+    mag = torch.zeros(v + 6, d, dtype=torch.float64, device="cuda:0").index_add_(0, t, x.double().abs() * 0.25)[:v]
+    k = torch.bincount(t, minlength=v)[:v, None]
+    ref[1] = mag[1] = 0
+    tol = (k + 3) * 2.0 ** -24 * 1.01 * mag
+    assert bool((torch.abs(dw.double() - ref) <= tol + (ref.abs() + tol) * 2.0 ** -8).all())
+    old = _draw((v, d), "f32", 64)
+    acc = embedding_backward(t.int(), x, v, 0.25, padding_idx=1, accumulate_into=old.clone())
+    tol = tol + (k + 3) * 2.0 ** -24 * old.double().abs()
+    assert bool((torch.abs(acc.double() - ref - old.double()) <= tol + (ref + old.double()).abs() * 2.0 ** -24).all())
+    untouched = (k[:, 0] == 0)
+    untouched[1] = True
+    assert torch.equal(acc[untouched], old[untouched]) and not dw[untouched].any()
+
+
 def test_gradient_of_no_tokens():
     import torch
     from paper_2605_21442_amd.training import embedding_backward
