@@ -3,10 +3,10 @@
 // is copied to the device beforehand, so a call can be captured and its table needs no storage.
 //
 // All of it is bound by memory on a whole model (1.2e9 bf16 elements): the 32-bit step with an fp32 master copy moves
-// 28 bytes an element in 6.52 ms (5.3 TB/s), the 8-bit step without 10.1 bytes in 2.55 to 2.63 ms (4.8 TB/s; its vector
-// instructions alone would take 2.0), the values of the 8-bit moments 6.1 bytes in 1.3 ms (5.7), the norm 2 bytes in
-// 0.40 ms (6.1). Hundreds of small tensors are bound by the launches' ramps (224 adapter tensors, 7.9e6 elements: 81 us in 5
-// launches, 3.9 TB/s) and by the host that gathers their addresses.
+// 28 bytes an element in 6.52 to 6.57 ms (5.3 TB/s), the 8-bit step without 10.1 bytes in 2.55 to 2.63 ms (4.8 TB/s; its
+// vector instructions alone would take 2.0), the values of the 8-bit moments 6.1 bytes in 1.3 ms (5.7), the norm 2 bytes in
+// 0.40 ms (6.1). Hundreds of small tensors are bound by the launches' ramps (224 adapter tensors, 7.9e6 elements: 67 us in 3
+// launches, 4.7 TB/s; in 5 launches 74) and, in the norm, by the host (15 us of kernels and 18 a call).
 #pragma once
 
 namespace {
