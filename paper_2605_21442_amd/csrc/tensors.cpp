@@ -28,22 +28,34 @@ const at::Tensor* plain(PyObject* o, int64_t device, int32_t* dtype) {
   return &t;
 }
 
-// describe(tensors, like, device, table, row_bytes, o_data, o_n, o_dtype) -> bool
+bool has_shape(const at::Tensor& t, PyObject* shape) {
+  if (!PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) != t.dim()) return false;
+  for (int64_t k = 0; k < t.dim(); ++k) {
+    const long long n = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, k));
+    if (n != t.size(k)) {
+      PyErr_Clear();       // (an entry that is no number is no size either)
+      return false;
+    }
+  }
+  return true;
+}
+
+// describe(tensors, shapes, device, table, row_bytes, o_data, o_n, o_dtype) -> bool
 // Writes each tensor's address (uint64 at o_data of its row of the table), element count (int64 at o_n, unless o_n < 0) and
-// type (int32 at o_dtype). like: None, or tensors whose shapes these must have. False, with the table half
-// written, where some tensor is not plain memory of the device or of that shape.
+// type (int32 at o_dtype). shapes: None, or the shape (a tuple) that each must have. False, with the table half
+// written, where some tensor is not plain memory of the device or not of its shape.
 PyObject* describe(PyObject*, PyObject* args) {
-  PyObject *list, *like;
+  PyObject *list, *shapes;
   Py_buffer table;
   long long device;
   Py_ssize_t row, o_data, o_n, o_dtype;
-  if (!PyArg_ParseTuple(args, "O!OLw*nnnn", &PyList_Type, &list, &like, &device, &table, &row, &o_data, &o_n, &o_dtype))
+  if (!PyArg_ParseTuple(args, "O!OLw*nnnn", &PyList_Type, &list, &shapes, &device, &table, &row, &o_data, &o_n, &o_dtype))
     return nullptr;
   const Py_ssize_t n = PyList_GET_SIZE(list);
   const auto fits = [row](Py_ssize_t at, Py_ssize_t size) { return at >= 0 && at + size <= row; };
   bool ok = true;
   if (row <= 0 || n > table.len / row || !fits(o_data, 8) || (o_n >= 0 && !fits(o_n, 8)) || !fits(o_dtype, 4) ||
-      (like != Py_None && (!PyList_Check(like) || PyList_GET_SIZE(like) != n))) {
+      (shapes != Py_None && (!PyList_Check(shapes) || PyList_GET_SIZE(shapes) != n))) {
     PyBuffer_Release(&table);
     PyErr_SetString(PyExc_ValueError, "table, offsets and lists do not fit together");
     return nullptr;
@@ -54,10 +66,7 @@ PyObject* describe(PyObject*, PyObject* args) {
       int32_t dtype;
       const at::Tensor* t = plain(PyList_GET_ITEM(list, i), device, &dtype);
       ok = t != nullptr;
-      if (ok && like != Py_None) {
-        PyObject* other = PyList_GET_ITEM(like, i);
-        ok = THPVariable_Check(other) && THPVariable_Unpack(other).sizes().equals(t->sizes());
-      }
+      if (ok && shapes != Py_None) ok = has_shape(*t, PyList_GET_ITEM(shapes, i));
       if (!ok) break;
       const uint64_t address = reinterpret_cast<uint64_t>(t->const_data_ptr());
       const int64_t count = t->numel();

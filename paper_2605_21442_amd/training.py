@@ -130,7 +130,9 @@ def embedding_backward(ids: torch.Tensor, grad_out: torch.Tensor, v: int, scale:
 
 
 class TokenEmbedding(torch.autograd.Function):
-    """Scaled lookup of rows by id; the backward returns the weight's gradient, dense."""
+    """Scaled lookup of rows by id; the backward returns the weight's gradient, dense. (To capture a training step into a
+    graph beside eager ones of the same weights, capture ``embedding_forward`` and ``embedding_backward``: torch's own
+    accumulation of a leaf's gradient may not move between a live eager graph and a capture.)"""
 
     @staticmethod
     def forward(ctx, ids, weight, scale=1.0, padding_idx=None):
@@ -263,9 +265,10 @@ class AdamWTensors:
         self.master = None
         if master_weights:
             self.master = torch.zeros(total, dtype=torch.float32, device=dev)
-            for p, o in zip(self.params, self.offsets):
-                self.master[o:o + p.numel()].copy_(p.detach().reshape(-1))
-        self._shapes = [torch.empty(p.shape, device="meta") for p in self.params]
+            with torch.no_grad():
+                for p, m in zip(self.params, self.master.split([-(-p.numel() // _BLOCK) * _BLOCK for p in self.params])):
+                    m[:p.numel()].view(p.shape).copy_(p)
+        self._shapes = [p.shape for p in self.params]
         size = self.exp_avg.element_size()
         t = np.zeros(len(self.params), dtype=_TENSOR)
         off = np.array(self.offsets, dtype=np.uint64)
@@ -307,7 +310,7 @@ class AdamWTensors:
                                _TENSOR.fields["grad_dtype"][1]):
             have = [k for k, g in enumerate(grads) if g is not None]
             grads, t = [grads[k] for k in have], t[have]     # (the tensors without a gradient are not in the call)
-            if any(g.shape != self._shapes[k].shape for g, k in zip(grads, have)):
+            if any(g.shape != self._shapes[k] for g, k in zip(grads, have)):
                 raise ValueError("gradients must be shaped like their parameters")
             grads, dtypes = _dense(grads, self.device.index)
             t["grad"] = [g.data_ptr() for g in grads]

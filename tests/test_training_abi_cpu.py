@@ -234,7 +234,7 @@ def test_describe_fills_a_table():
     assert t["data"].tolist() == [a.data_ptr() for a in ts] and t["n"].tolist() == [100, 4, 6, 5, 0]
     assert t["dtype"].tolist() == [0, 0, 1, 1, 1] and (t["pad"] == 77).all()
     t["n"] = -5
-    assert _native().describe(ts, [torch.empty(a.shape, device="meta") for a in ts], -1, t, TABLE.itemsize, 8, -1, 20)
+    assert _native().describe(ts, [a.shape for a in ts], -1, t, TABLE.itemsize, 8, -1, 20)
     assert (t["n"] == -5).all()                        # not asked for
     assert _native().stand_at(ts, t, TABLE.itemsize, 8) and not _native().stand_at(ts[1:], t, TABLE.itemsize, 8)
     assert _native().describe([], None, -1, t, TABLE.itemsize, 8, 0, 20)
@@ -251,8 +251,8 @@ def test_describe_leaves_to_the_caller_what_is_not_plain_memory():
     for x in bad:
         assert not _native().describe([good, x], None, -1, t, TABLE.itemsize, 8, 0, 20), type(x)
     assert not _native().describe([good], None, 0, t, TABLE.itemsize, 8, 0, 20)          # not on that device
-    assert not _native().describe([good], [torch.zeros(16)], -1, t, TABLE.itemsize, 8, 0, 20)   # another shape
-    assert not _native().describe([good], [None], -1, t, TABLE.itemsize, 8, 0, 20)
+    for shape in [(16,), (4, 4, 1), (4, 5), (4, "x"), (4, None), [4, 4], None, ()]:
+        assert not _native().describe([good], [shape], -1, t, TABLE.itemsize, 8, 0, 20), shape
 
 
 def test_describe_refuses_a_table_that_does_not_fit():
