@@ -214,7 +214,7 @@ struct EmbedIds {
   int64_t n, v_begin, v, padding;
 };
 
-constexpr int64_t kKeptBytes = (int64_t)192 << 20;    // of a lookup's output, at most, that is kept
+constexpr int64_t kKeptBytes = (int64_t)192 << 20;    // of an output, at most, that is kept in the caches
 
 template <typename T, bool kOnce>
 __global__ __launch_bounds__(256) void k_embed_lookup(EmbedIds e, int64_t v_total, const T* __restrict__ W, int64_t ldw,
@@ -509,9 +509,13 @@ __global__ __launch_bounds__(256) void k_embed_few(EmbedRows e, const T* __restr
   grad_store<TW, kAdd>(o, old, sum, scale);
 }
 
+// kOnce: past the caches, which a dW larger than they are would only empty of dOut (16384 tokens, 128256 x 4096: 213 -> 202 us)
+template <bool kOnce>
 __global__ __launch_bounds__(256) void k_embed_zero(char* __restrict__ dw, int64_t bytes) {
   const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 16;
-  if (at < bytes) store16_padded(dw + at, i32x4_t{0, 0, 0, 0});
+  if (at >= bytes) return;
+  if (kOnce) store16_padded_nt(dw + at, i32x4_t{0, 0, 0, 0});
+  else store16_padded(dw + at, i32x4_t{0, 0, 0, 0});
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -575,6 +579,11 @@ void launch_lookup(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, c
     (const T*)W, pl.ldw, (int)p->d, p->scale, (T*)out, status);
 }
 
+void launch_zero(Launcher& L, void* dw, int64_t bytes) {
+  L(K_EMBED_GRAD, bytes <= kKeptBytes ? k_embed_zero<false> : k_embed_zero<true>, dim3((unsigned)((bytes + 4095) / 4096)),
+    dim3(256), (char*)dw, bytes);
+}
+
 template <typename T, typename TW, bool kAdd>
 void launch_embed_grad(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedSorted& s, const void* dout,
                        void* dw, float* parts) {
@@ -584,7 +593,7 @@ void launch_embed_grad(Launcher& L, const lce_embedding_t* p, const EmbedPlan& p
   // 35 against 33; 16384, 32000 x 4096: 106 against 103; 65536, 128256 x 4096 of even ids: 406 against 363)
   const bool zero = !kAdd && p->n <= p->v / 4 && bytes >= (int64_t)256 << 20;
   const int64_t fill = kAdd || zero ? 0 : (bytes + kFillBytes - 1) / kFillBytes;
-  if (zero) L(K_EMBED_GRAD, k_embed_zero, dim3((unsigned)((bytes + 4095) / 4096)), dim3(256), (char*)dw, bytes);
+  if (zero) launch_zero(L, dw, bytes);
   L(K_EMBED_GRAD, k_embed_grad<T, TW, kAdd>, dim3((unsigned)((units + 3) / 4)), dim3(256), s, (const T*)dout, pl.ldx,
     (int)p->d, pl.per, units, pl.slices, p->scale, (TW*)dw, parts);
   L(K_EMBED_GRAD, k_embed_join<TW, kAdd>, dim3((unsigned)(join + fill)), dim3(256), s, (int)p->v, (int)p->d, pl.per,
@@ -599,7 +608,7 @@ inline bool few_tokens(const lce_embedding_t* p, const EmbedPlan& pl) {
 template <typename T, typename TW, bool kAdd>
 void launch_embed_few(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedRows& e, const void* dout, void* dw) {
   const int64_t bytes = p->v * p->d * (int64_t)sizeof(TW);
-  if (!kAdd) L(K_EMBED_GRAD, k_embed_zero, dim3((unsigned)((bytes + 4095) / 4096)), dim3(256), (char*)dw, bytes);
+  if (!kAdd) launch_zero(L, dw, bytes);
   L(K_EMBED_GRAD, p->id_bytes == 8 ? k_embed_few<T, TW, kAdd, 8> : k_embed_few<T, TW, kAdd, 4>,
     dim3((unsigned)(p->n * pl.slices)), dim3(256), e, (const T*)dout, pl.ldx, (int)p->d, pl.slices, p->scale, (TW*)dw);
 }
