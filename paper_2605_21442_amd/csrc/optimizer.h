@@ -5,7 +5,7 @@
 // All of it is bound by memory on a whole model (1.2e9 bf16 elements): the 32-bit step with an fp32 master copy moves
 // 28 bytes an element in 6.52 to 6.57 ms (5.3 TB/s), the 8-bit step without 10.1 bytes in 2.55 to 2.63 ms (4.8 TB/s; its
 // vector instructions alone would take 2.0), the values of the 8-bit moments 6.1 bytes in 1.3 ms (5.7), the norm 2 bytes in
-// 0.40 ms (6.1). Hundreds of small tensors are bound by the launches' ramps (224 adapter tensors, 7.9e6 elements: 67 us in 3
+// 0.40 ms (6.1). Hundreds of small tensors are bound by the launches' ramps (224 adapter tensors, 11.3e6 elements: 67 us in 3
 // launches, 4.7 TB/s; in 5 launches 74) and, in the norm, by the host (15 us of kernels and 18 a call).
 #pragma once
 
@@ -493,10 +493,12 @@ template <int kBits>
 void launch_adamw(Launcher& L, const lce_adamw_tensor_t* tensors, int64_t count, const lce_adamw_t* groups, int64_t total,
                   const float* grad_scale, uint32_t seed) {
   AdamWTable<kBits> t;
-  // elements of a workgroup: one round (1024 or 2048), for enough workgroups to fill the card, or up to 8192 where there are
-  // more than 8192 of them, each of which first finds its tensor
+  // elements of a workgroup. 32-bit moments: one round, so that the workgroups go through the addresses in order (1.2e9
+  // elements 5.80 ms; 2048, 4096, 8192 a workgroup: 6.24, 6.31, 6.54). 8-bit ones, which the vector units bound as much: one
+  // round (2048) to fill the card, or up to 16384 where there are more than 8192 workgroups, each of which first finds
+  // its tensor (1.2e9 elements 2.34 ms, with 2048: 2.49; 5.3e6 elements 28 us with 8192, 25 with 2048)
   t.per = kBits == 8 ? 2048 : 1024;
-  while (t.per < 8192 && total > (int64_t)8192 * t.per) t.per *= 2;
+  while (kBits == 8 && t.per < 16384 && total > (int64_t)8192 * t.per) t.per *= 2;
   int32_t group_of[kTableGroups];
   int n_groups = 0;
   int64_t blocks = 0;
