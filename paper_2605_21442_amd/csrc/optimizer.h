@@ -3,10 +3,10 @@
 // is copied to the device beforehand, so a call can be captured and its table needs no storage.
 //
 // All of it is bound by memory on a whole model (1.2e9 bf16 elements): the 32-bit step with an fp32 master copy moves
-// 28 bytes an element in 6.52 to 6.57 ms (5.3 TB/s), the 8-bit step without 10.1 bytes in 2.55 to 2.63 ms (4.8 TB/s; its
+// 28 bytes an element in 5.6 to 5.9 ms (5.9 to 6.2 TB/s), the 8-bit step without 10.1 bytes in 2.55 to 2.63 ms (4.8 TB/s; its
 // vector instructions alone would take 2.0), the values of the 8-bit moments 6.1 bytes in 1.3 ms (5.7), the norm 2 bytes in
-// 0.40 ms (6.1). Hundreds of small tensors are bound by the launches' ramps (224 adapter tensors, 11.3e6 elements: 67 us in 3
-// launches, 4.7 TB/s; in 5 launches 74) and, in the norm, by the host (15 us of kernels and 18 a call).
+// 0.40 ms (6.1). Hundreds of small tensors are bound by the launches' ramps (224 adapter tensors, 11.3e6 elements: 64 us in 3
+// launches, 4.9 TB/s; in 5 launches 74) and, in the norm, by the host (15 us of kernels and 18 a call).
 #pragma once
 
 namespace {
@@ -59,7 +59,7 @@ __device__ __forceinline__ int table_entry(const Entry* e, int count, uint32_t b
 
 // N consecutive elements from i on as fp32, and back; elements at or past n are 0 and are not touched. `wide`: the
 // tensor's address is a multiple of 16 bytes (i is a multiple of N). Both pass the L2 by: a step touches every byte once
-// (1.2e9 elements, 32-bit moments: 6.72 -> 6.57 ms; adapters 117 -> 107 us).
+// (1.2e9 elements, 32-bit moments, 8192 a workgroup: 6.72 -> 6.57 ms; adapters 117 -> 107 us).
 template <int N>
 __device__ __forceinline__ void load_elems(const void* p, int64_t i, int64_t n, bool f32, bool wide, float x[N]) {
   if (wide && i + N <= n) {
