@@ -14,6 +14,7 @@ import math
 
 import numpy as np
 import torch
+from torch.autograd.forward_ad import unpack_dual
 from torch.autograd.function import once_differentiable
 from torch.autograd.graph import increment_version
 
@@ -154,8 +155,8 @@ def token_embedding(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0,
                     padding_idx: int | None = None) -> torch.Tensor:
     """``scale * weight[ids]``: the token embedding, with a gradient for the weight [V, D] (bf16 or fp32). Tokens
     of ``padding_idx`` give no gradient. An id outside the vocabulary gives a row of zeros and no gradient
-    (``embedding_forward`` also reports it)."""
-    if not (weight.requires_grad and torch.is_grad_enabled()):
+    (``embedding_forward`` also reports it). Forward-mode derivatives are refused."""
+    if not (weight.requires_grad and torch.is_grad_enabled()) and unpack_dual(weight).tangent is None:
         return embedding_forward(ids, weight, scale, padding_idx, want_status=False)[0]
     return TokenEmbedding.apply(ids, weight, scale, padding_idx)
 
