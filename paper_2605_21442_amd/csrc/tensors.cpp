@@ -81,21 +81,39 @@ PyObject* describe(PyObject*, PyObject* args) {
   return PyBool_FromLong(ok);
 }
 
-// stand_at(tensors, table, row_bytes, o_data) -> bool: whether each tensor still has the address in its row.
+// Whether t is `count` elements of a type (bf16 0, fp32 1) one after the other, all within its storage.
+bool lies_whole(const at::Tensor& t, int64_t count, int32_t dtype) {
+  if (!t.defined() || t.layout() != at::kStrided || t.unsafeGetTensorImpl()->is_python_dispatch()) return false;
+  if (t.scalar_type() != (dtype == 1 ? at::kFloat : at::kBFloat16)) return false;
+  return t.has_storage() && t.is_contiguous() && !t.is_neg() && t.numel() == count &&
+         (t.storage_offset() + count) * static_cast<int64_t>(t.element_size()) <= static_cast<int64_t>(t.storage().nbytes());
+}
+
+// stand_at(tensors, table, row_bytes, o_data, o_n = -1, o_dtype = -1) -> bool: whether each tensor still has the address
+// in its row and, with o_n and o_dtype, is still as many elements of that type without gaps.
 PyObject* stand_at(PyObject*, PyObject* args) {
   PyObject* list;
   Py_buffer table;
-  Py_ssize_t row, o_data;
-  if (!PyArg_ParseTuple(args, "O!y*nn", &PyList_Type, &list, &table, &row, &o_data)) return nullptr;
+  Py_ssize_t row, o_data, o_n = -1, o_dtype = -1;
+  if (!PyArg_ParseTuple(args, "O!y*nn|nn", &PyList_Type, &list, &table, &row, &o_data, &o_n, &o_dtype)) return nullptr;
   const Py_ssize_t n = PyList_GET_SIZE(list);
-  bool ok = row > 0 && n <= table.len / row && o_data >= 0 && o_data + 8 <= row;
+  bool ok = row > 0 && n <= table.len / row && o_data >= 0 && o_data + 8 <= row && o_n + 8 <= row && o_dtype + 4 <= row &&
+            (o_n < 0) == (o_dtype < 0);
   try {
     const char* at = static_cast<const char*>(table.buf);
     for (Py_ssize_t i = 0; ok && i < n; ++i, at += row) {
       PyObject* o = PyList_GET_ITEM(list, i);
       uint64_t address;
       std::memcpy(&address, at + o_data, 8);
-      ok = THPVariable_Check(o) && reinterpret_cast<uint64_t>(THPVariable_Unpack(o).const_data_ptr()) == address;
+      ok = THPVariable_Check(o);
+      if (ok && o_n >= 0) {
+        int64_t count;
+        int32_t dtype;
+        std::memcpy(&count, at + o_n, 8);
+        std::memcpy(&dtype, at + o_dtype, 4);
+        ok = lies_whole(THPVariable_Unpack(o), count, dtype);
+      }
+      ok = ok && reinterpret_cast<uint64_t>(THPVariable_Unpack(o).const_data_ptr()) == address;
     }
   } catch (const std::exception&) {
     ok = false;

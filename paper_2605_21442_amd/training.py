@@ -298,8 +298,9 @@ class AdamWTensors:
         was captured with in every replay."""
         params = self.params
         native = _native()
-        if not native.stand_at(params, self._table, _TENSOR.itemsize, _TENSOR.fields["param"][1]):
-            raise ValueError("a parameter's storage has changed since the state was made")
+        if len(params) != len(self._table) or not native.stand_at(params, self._table, _TENSOR.itemsize,
+                                                                  *(_TENSOR.fields[k][1] for k in ("param", "n", "param_dtype"))):
+            raise ValueError("a parameter's storage, type or layout has changed since the state was made")
         grads = [p.grad for p in params] if grads is None else list(grads)
         if len(grads) != len(params):
             raise ValueError(f"{len(grads)} gradients for {len(params)} parameters")
