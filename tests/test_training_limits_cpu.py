@@ -44,3 +44,19 @@ def test_tensors_that_stand_where_they_did_but_lie_otherwise_are_noticed():
         assert not stands(bad)
     for offsets in ((8, -1, 20), (8, 0, -1), (8, 17, 20), (8, 0, 21), (20, 0, 20)):
         assert not _native().stand_at([p], t, TABLE.itemsize, *offsets), offsets
+
+
+def test_a_subclass_with_memory_of_its_own_stands_too():
+    import torch
+    from paper_2605_21442_amd.training import _native
+
+    class Logged(torch.Tensor):
+        @classmethod
+        def __torch_dispatch__(cls, func, types, args=(), kwargs=None):
+            with torch._C._DisableTorchDispatch():
+                return func(*args, **(kwargs or {}))
+
+    p = torch.zeros(6, 6)
+    t = np.zeros(1, dtype=TABLE)
+    assert _native().describe([p], None, -1, t, TABLE.itemsize, 8, 0, 20)
+    assert _native().stand_at([p.as_subclass(Logged)], t, TABLE.itemsize, 8, 0, 20)
