@@ -81,9 +81,10 @@ PyObject* describe(PyObject*, PyObject* args) {
   return PyBool_FromLong(ok);
 }
 
-// Whether t is `count` elements of a type (bf16 0, fp32 1) one after the other, all within its storage.
+// Whether t is `count` elements of a type (bf16 0, fp32 1, bytes 2) one after the other, all within its storage.
 bool lies_whole(const at::Tensor& t, int64_t count, int32_t dtype) {
-  if (!t.defined() || t.layout() != at::kStrided || t.scalar_type() != (dtype == 1 ? at::kFloat : at::kBFloat16)) return false;
+  if (!t.defined() || t.layout() != at::kStrided || t.scalar_type() != (dtype == 2 ? at::kByte : dtype == 1 ? at::kFloat : at::kBFloat16))
+    return false;
   return t.has_storage() && t.is_contiguous() && !t.is_neg() && t.numel() == count &&
          (t.storage_offset() + count) * static_cast<int64_t>(t.element_size()) <= static_cast<int64_t>(t.storage().nbytes());
 }

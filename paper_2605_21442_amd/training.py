@@ -219,7 +219,8 @@ class AdamWTensors:
     The state is flat: tensor i stands at ``offsets[i]`` of ``exp_avg``, ``exp_avg_sq`` and ``master``, in whole blocks
     of 32 elements. ``state_bits=8`` holds each moment in a byte per element and a unit byte per block
     (``exp_avg``, ``exp_avg_root``, ``units`` [blocks, 2]; the form is described at lce_adamw_tensors_step);
-    its rounding draws on ``seed`` and the step count."""
+    its rounding draws on ``seed`` and the step count. These tensors may be replaced or moved between steps by others of
+    their type and size on the same device."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                  master_weights: bool = False, state_bits: int = 32, seed: int = 0):
@@ -270,21 +271,42 @@ class AdamWTensors:
                 for p, m in zip(self.params, self.master.split([-(-p.numel() // _BLOCK) * _BLOCK for p in self.params])):
                     m[:p.numel()].view(p.shape).copy_(p)
         self._shapes = [p.shape for p in self.params]
-        size = self.exp_avg.element_size()
         t = np.zeros(len(self.params), dtype=_TENSOR)
-        off = np.array(self.offsets, dtype=np.uint64)
         t["param"] = [p.data_ptr() for p in self.params]
-        t["exp_avg"] = self.exp_avg.data_ptr() + off * size
-        t["exp_avg_sq"] = second.data_ptr() + off * size
-        if self.units is not None:
-            t["units"] = self.units.data_ptr() + off // 16
-        if master_weights:
-            t["master"] = [self.master.data_ptr() + 4 * o if p.dtype == torch.bfloat16 else 0
-                           for p, o in zip(self.params, self.offsets)]
         t["n"] = [p.numel() for p in self.params]
-        t["place"], t["group"] = off, at
+        t["place"], t["group"] = self.offsets, at
         t["param_dtype"] = [_DTYPES[p.dtype] for p in self.params]
         self._table = t
+        self._names = ["exp_avg"] + (["exp_avg_sq"] if state_bits == 32 else ["exp_avg_root", "units"])
+        self._names += ["master"] if master_weights else []
+        self._forms = [(getattr(self, k).shape, getattr(self, k).dtype) for k in self._names]
+        self._address_state()
+
+    def _address_state(self) -> None:
+        """The addresses of the state's tensors, into the table of the call."""
+        state = [getattr(self, k) for k in self._names]
+        for k, x, (shape, dtype) in zip(self._names, state, self._forms):
+            if not (isinstance(x, torch.Tensor) and x.shape == shape and x.dtype == dtype and x.device == self.device
+                    and x.is_contiguous() and not x.is_neg()
+                    and (x.storage_offset() + x.numel()) * x.element_size() <= x.untyped_storage().nbytes()):
+                raise ValueError(f"{k} must be a contiguous {dtype} tensor of {tuple(shape)} on {self.device}, since it is updated "
+                                 "in place")
+        t, off, at = self._table, self._table["place"].astype(np.uint64), {k: x.data_ptr() for k, x in zip(self._names, state)}
+        t["exp_avg"] = at["exp_avg"] + off * state[0].element_size()
+        t["exp_avg_sq"] = at[self._names[1]] + off * state[1].element_size()
+        if "units" in at:
+            t["units"] = at["units"] + off // 16
+        if "master" in at:
+            t["master"] = np.where(t["param_dtype"] == B.LCE_DTYPE_BF16, at["master"] + 4 * off, 0)
+        self._state_table = np.zeros(len(state), dtype=_GRAD)
+        self._state_table["data"] = list(at.values())
+        self._state_table["n"] = [x.numel() for x in state]
+        self._state_table["dtype"] = [2 if x.dtype == torch.uint8 else _DTYPES[x.dtype] for x in state]
+
+    def _check_state(self) -> None:
+        """Follows the state's tensors where they were replaced or moved (a checkpoint, offloading) since the last call."""
+        if not _native().stand_at([getattr(self, k) for k in self._names], self._state_table, _GRAD.itemsize, 0, 8, 16):
+            self._address_state()
 
     def _seed_of(self, step: int) -> int:
         return (self.seed * 0x9E3779B9 + step * 0x6A09E667) & 0xFFFFFFFF
@@ -301,6 +323,7 @@ class AdamWTensors:
         if len(params) != len(self._table) or not native.stand_at(params, self._table, _TENSOR.itemsize,
                                                                   *(_TENSOR.fields[k][1] for k in ("param", "n", "param_dtype"))):
             raise ValueError("a parameter's storage, type or layout has changed since the state was made")
+        self._check_state()
         grads = [p.grad for p in params] if grads is None else list(grads)
         if len(grads) != len(params):
             raise ValueError(f"{len(grads)} gradients for {len(params)} parameters")
@@ -332,6 +355,7 @@ class AdamWTensors:
         (lce_adamw_moments)."""
         if self.state_bits != 8:
             raise ValueError("32-bit moments are exp_avg and exp_avg_sq themselves")
+        self._check_state()
         first = torch.empty(self.exp_avg.shape, dtype=torch.bfloat16, device=self.device)
         root = torch.empty_like(first)
         with _on(self.device):

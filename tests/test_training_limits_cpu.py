@@ -1,7 +1,43 @@
 """Token embedding, AdamW over many tensors and gradient norm without a GPU: calls at the edge of what they take, which
 are answered rightly or refused. Where a call would reach the device, a stand-in takes the library's place."""
+import ctypes
+import types
+
 import numpy as np
 import pytest
+
+
+class OnGpu:
+    """Host tensors that AdamWTensors takes for parameters, and the calls that it makes of the library: for each its table of
+    tensors, its constants, and its bits."""
+
+    def __init__(self, monkeypatch):
+        import torch
+        from paper_2605_21442_amd import training as TR
+        native = TR._native()
+        here = types.SimpleNamespace(stand_at=native.stand_at, changed=native.changed,
+                                     describe=lambda tensors, shapes, device, *a: native.describe(tensors, shapes, -1, *a))
+
+        class Param(torch.Tensor):
+            is_cuda = property(lambda self: True)
+
+        def call(table, count, groups, n_groups, bits, scale, seed, stream):
+            rows = (ctypes.c_char * (count * TR._TENSOR.itemsize)).from_address(table)
+            opts = [TR.B.LceAdamW.from_address(groups + k * ctypes.sizeof(TR.B.LceAdamW)) for k in range(n_groups)]
+            self.calls.append((np.frombuffer(bytes(rows), dtype=TR._TENSOR),
+                               [{f: getattr(o, f) for f, _ in o._fields_} for o in opts], bits))
+
+        self.calls, self.param = [], lambda *shape: torch.zeros(*shape).as_subclass(Param)
+        monkeypatch.setattr(TR, "_native", lambda: here)
+        monkeypatch.setattr(TR, "_stream", lambda dev: 0)
+        monkeypatch.setattr(TR, "_on", lambda dev: TR._HERE)
+        monkeypatch.setattr(TR.B, "lce_adamw_tensors_step",
+                            lambda t, n, g, *a: call(t, n, ctypes.addressof(g) if isinstance(g, ctypes.Array) else g, *a))
+
+
+@pytest.fixture
+def on_gpu(monkeypatch):
+    return OnGpu(monkeypatch)
 
 
 @pytest.mark.parametrize("grad_enabled", [True, False])
@@ -60,3 +96,51 @@ def test_a_subclass_with_memory_of_its_own_stands_too():
     t = np.zeros(1, dtype=TABLE)
     assert _native().describe([p], None, -1, t, TABLE.itemsize, 8, 0, 20)
     assert _native().stand_at([p.as_subclass(Logged)], t, TABLE.itemsize, 8, 0, 20)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_follows_the_state_where_it_was_moved(on_gpu, bits):
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    ps = [on_gpu.param(40), on_gpu.param(3, 5)]
+    ps[1] = ps[1].bfloat16()
+    opt = AdamWTensors(ps, state_bits=bits, master_weights=True)
+    names = ["exp_avg", "exp_avg_sq", "master"] if bits == 32 else ["exp_avg", "exp_avg_root", "units", "master"]
+    gs = [torch.ones(40), torch.ones(3, 5)]
+
+    def addresses_are_the_states():
+        t = on_gpu.calls[-1][0]
+        size = bits // 8
+        for k, off in enumerate(opt.offsets):
+            assert t["exp_avg"][k] == opt.exp_avg.data_ptr() + off * size
+            assert t["exp_avg_sq"][k] == getattr(opt, names[1]).data_ptr() + off * size
+            assert t["units"][k] == (opt.units.data_ptr() + off // 16 if bits == 8 else 0)
+        assert t["master"].tolist() == [0, opt.master.data_ptr() + 4 * opt.offsets[1]]     # (of the bf16 tensor)
+
+    opt.step(gs)
+    addresses_are_the_states()
+    for name in names:
+        before = getattr(opt, name).data_ptr()
+        setattr(opt, name, getattr(opt, name).clone())
+        opt.step(gs)
+        assert getattr(opt, name).data_ptr() != before
+        addresses_are_the_states()
+        getattr(opt, name).data = getattr(opt, name).clone()
+        opt.step(gs)
+        addresses_are_the_states()
+    done = len(on_gpu.calls)
+    for name in names:
+        own = getattr(opt, name)
+        freed = own.clone()
+        freed.untyped_storage().resize_(0)
+        for bad in (None, own[:-1], own.view(-1)[1:], own.to(torch.float64), own.to("meta"), freed, "no tensor"):
+            setattr(opt, name, bad)
+            with pytest.raises(ValueError, match=name):
+                opt.step(gs)
+            if bits == 8:
+                with pytest.raises(ValueError, match=name):
+                    opt.moments()
+        setattr(opt, name, own)
+    assert len(on_gpu.calls) == done
+    opt.step(gs)
+    addresses_are_the_states()
