@@ -459,7 +459,9 @@ lce_status_t lce_embedding_backward(const lce_embedding_t* p, const void* ids, c
 
 /*
  * One AdamW step over many tensors (a whole model's, or its adapters'), with the arithmetic of
- * lce_adamw_step element by element: the same bits for bf16 tensors with 32-bit moments. Each tensor is n contiguous elements.
+ * lce_adamw_step element by element: the same bits for bf16 tensors with 32-bit moments, and with 8-bit ones the same formula
+ * from the moments that they stand for, root and quotient within one unit in the last place of the rounded ones. Each tensor
+ * is n contiguous elements.
  *   param          bf16 or fp32, updated in place
  *   grad           bf16 or fp32, or NULL for a zero gradient
  *   exp_avg, exp_avg_sq, units: the moments, updated in place (16-byte aligned, units 2). state_bits 32: fp32 [n]
@@ -480,7 +482,9 @@ lce_status_t lce_embedding_backward(const lce_embedding_t* p, const void* ids, c
  * neighbouring codes with the probability of the value's place between them, so that a moment that moves
  * by less than a code a step (beta2 near 1) still moves by as much on average. The 16 random bits of an
  * element come from a hash of (place + index, seed), so a call is deterministic in its arguments. A
- * nonzero root is held as at least the smallest code. The update itself uses the fp32 moments.
+ * nonzero root is held as at least the smallest code. The update itself uses the fp32 moments. Where the second
+ * moment overflows in fp32 the element takes no update, as in lce_adamw_step, but its finite root is held: gradients
+ * that are finite leave moments that are (at most 1.875 * 2^127 and 1.9375 * 2^127).
  *
  *   grad_scale     device fp32 [1] or NULL: every gradient is multiplied by it first. If it is not finite
  *                  the call changes nothing (a step with overflowed gradients is skipped on the device).

@@ -57,6 +57,10 @@ __device__ __forceinline__ int table_entry(const Entry* e, int count, uint32_t b
   return __builtin_amdgcn_readfirstlane(k);
 }
 
+__device__ __forceinline__ float load_elem(const void* p, int64_t i, bool f32) {
+  return f32 ? ((const float*)p)[i] : bf16_to_f32(((const uint16_t*)p)[i]);
+}
+
 // N consecutive elements from i on as fp32, and back; elements at or past n are 0 and are not touched. `wide`: the
 // tensor's address is a multiple of 16 bytes (i is a multiple of N). Both pass the L2 by: a step touches every byte once
 // (1.2e9 elements, 32-bit moments, 8192 a workgroup: 6.72 -> 6.57 ms; adapters 117 -> 107 us).
@@ -79,8 +83,7 @@ __device__ __forceinline__ void load_elems(const void* p, int64_t i, int64_t n, 
     return;
   }
 #pragma unroll
-  for (int k = 0; k < N; ++k)
-    x[k] = i + k >= n ? 0.f : f32 ? ((const float*)p)[i + k] : bf16_to_f32(((const uint16_t*)p)[i + k]);
+  for (int k = 0; k < N; ++k) x[k] = i + k >= n ? 0.f : load_elem(p, i + k, f32);
 }
 
 template <int N>
@@ -154,34 +157,65 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
   return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));   // lanes 2 3 0 1
 }
 
-// 8 elements' moments from their bytes. A block of NaN has its codes' exponent bits all set.
+// What a byte of the first moment (a sign and a 7-bit code) and one of the root stand for. A block of NaN has its codes'
+// exponent bits all set.
+__device__ __forceinline__ float decode_first(uint32_t byte, int sm) {
+  const int c = (int)(byte << 24) >> 4;           // sign, copies of it, code
+  return ldexpf(__uint_as_float(((uint32_t)c & 0x87F00000u) | (sm == 255 ? 0x7FC00000u : 0u)), code_exponent<3>(sm));
+}
+__device__ __forceinline__ float decode_root(uint32_t byte, int sr) {
+  return ldexpf(__uint_as_float(byte << 19 | (sr == 255 ? 0x7FC00000u : 0u)), code_exponent<4>(sr));
+}
+
+// 8 elements' moments from their bytes
 __device__ __forceinline__ void decode_moments(const uint2 cm, const uint2 cr, int sm, int sr, float m[8], float r[8]) {
-  const uint32_t nan_m = sm == 255 ? 0x7FC00000u : 0, nan_r = sr == 255 ? 0x7FC00000u : 0;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const uint32_t wm = k < 4 ? cm.x : cm.y, wr = k < 4 ? cr.x : cr.y;
-    const int c = (int)(wm << (24 - 8 * (k & 3))) >> 4;           // sign, copies of it, 7-bit code
-    m[k] = ldexpf(__uint_as_float(((uint32_t)c & 0x87F00000u) | nan_m), code_exponent<3>(sm));
-    r[k] = ldexpf(__uint_as_float((wr >> (8 * (k & 3)) & 255u) << 19 | nan_r), code_exponent<4>(sr));
+    m[k] = decode_first(wm >> (8 * (k & 3)), sm);
+    r[k] = decode_root(wr >> (8 * (k & 3)) & 255u, sr);
   }
 }
 
-// AdamW's update of one element as adamw_update has it, but for the root and the quotient: each is the hardware's estimate
-// (1 ulp) with one Newton step, which is the correctly rounded value but for a few in a million. The compiler's own
-// sequences, which are right for every operand, made the 8-bit step bound by the vector units (91 instructions an
-// element, 3.04 ms for 1.2e9). v is 0 or at least 2^-126 where |g| > 1e-17; a smaller one has too small a root, which eps
-// hides. Where v or the quotient overflows, the result is NaN. Returns the root.
-__device__ __forceinline__ float adamw_update_near(float& p, float& m, float r, float g, const AdamWConst& c) {
+// The parameter's update of 8-bit states from the new moments: adamw_update's, but for the root and the quotient. Each is
+// the hardware's estimate (1 ulp) with one Newton step, which is the correctly rounded value but for a few in a million. The
+// compiler's own sequences, which are right for every operand, made the 8-bit step bound by the vector units (91
+// instructions an element, 3.04 ms for 1.2e9). The short form is for v = 0 or normal, eps within 2^+-100 and |m| < 2^27, so that
+// no estimate, product or quotient leaves the normal numbers (but a quotient too small to matter). Returns the root.
+__device__ __forceinline__ float adamw_step_near(float& p, float m, float v, const AdamWConst& c) {
 #pragma clang fp contract(off)
   p = p * c.keep;
-  m = c.beta1 * m + c.omb1 * g;
-  const float v = c.beta2 * (r * r) + c.omb2 * (g * g);
   const float y = __builtin_amdgcn_rsqf(fmaxf(v, 0x1p-126f)), root0 = v * y;
   const float root = fmaf(fmaf(-root0, root0, v), 0.5f * y, root0);
   const float denom = root * c.inv_sqrt_bc2 + c.eps;
   const float z = __builtin_amdgcn_rcpf(denom), q = m * z;
   p = p - c.step_size * fmaf(fmaf(-denom, q, m), z, q);
   return root;
+}
+
+// The same for all other operands, bit for bit adamw_update's parameter: a v that overflows gives no update. The root that is
+// held is then formed from scaled terms, so that gradients that are finite leave moments that are (those in the last 1/16 and
+// 1/32 below 2^128, whose code could round to infinity, are held as the largest code there; and beta2 = 0 takes nothing of
+// an r whose square overflows). It starts from the element's values in memory: kept in registers until here, the kernel
+// had 81 to 103 of them instead of 61, and every step took 3 % longer. A tensor of such operands alone takes 2.2 times as long.
+__device__ __forceinline__ void adamw_element_far(const AdamWEntry<8>& e, const AdamWConst& c, int64_t i, float scale, bool scaled,
+                                                  int s, float& p, float& m, float& r) {
+#pragma clang fp contract(off)
+  const float old = decode_root(((const uint8_t*)e.v)[i], s >> 8);
+  float g = e.grad ? load_elem(e.grad, i, e.grad_f32) : 0.f;
+  if (scaled) g = g * scale;
+  m = c.beta1 * decode_first(((const uint8_t*)e.m)[i], s & 255) + c.omb1 * g;
+  float v = c.beta2 * (old * old) + c.omb2 * (g * g);
+  if (v != v && old < INFINITY) v = c.omb2 * (g * g);
+  r = sqrtf(v);
+  p = (e.master ? e.master[i] : load_elem(e.param, i, e.param_f32)) * c.keep;
+  p = p - c.step_size * (m / (r * c.inv_sqrt_bc2 + c.eps));
+  if (v == INFINITY) {
+    const float a = old * 0x1p-65f, b = g * 0x1p-65f;
+    r = sqrtf(c.beta2 * (a * a) + c.omb2 * (b * b)) * 0x1p65f;
+    if (r < INFINITY) r = fminf(r, 0x1.Fp127f);
+  }
+  if (fabsf(m) < INFINITY) m = fminf(fmaxf(m, -0x1.Ep127f), 0x1.Ep127f);
 }
 
 // 32-bit moments: 4 elements per thread and round, so that every access of a wave is contiguous.
@@ -232,12 +266,35 @@ __device__ __forceinline__ void adamw_round8(const AdamWEntry<8>& e, const AdamW
     decode_moments(cm, cr, s & 255, s >> 8, m, r);
   }
   uint32_t am = 0, ar = 0;          // (elements at or past n have zero moments and gradients)
+  bool far = !(c.eps >= 0x1p-100f && c.eps <= 0x1p100f);
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     if (scaled) g[k] = g[k] * scale;
-    r[k] = adamw_update_near(p[k], m[k], r[k], g[k], c);
+    m[k] = c.beta1 * m[k] + c.omb1 * g[k];
+    const float v = c.beta2 * (r[k] * r[k]) + c.omb2 * (g[k] * g[k]);
+    far |= __builtin_amdgcn_classf(v, 0x283);          // positive and subnormal, infinite or NaN
+    r[k] = adamw_step_near(p[k], m[k], v, c);
     am = max(am, __float_as_uint(m[k]) & 0x7FFFFFFFu);
     ar = max(ar, __float_as_uint(r[k]) & 0x7FFFFFFFu);
+  }
+  far |= am >= 0x4D000000u;                            // 2^27
+  if (far) {
+    am = ar = 0;
+#pragma unroll 1                    // (the address is hidden from the compiler, which would keep one of each array in registers)
+    for (int n = 0; n < 8 && i + n < e.n; ++n) {
+      float p0, m0, r0;
+      int64_t at = i + n;
+      asm volatile("" : "+v"(at));
+      adamw_element_far(e, c, at, scale, scaled, s, p0, m0, r0);
+      am = max(am, __float_as_uint(m0) & 0x7FFFFFFFu);
+      ar = max(ar, __float_as_uint(r0) & 0x7FFFFFFFu);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        p[k] = k == n ? p0 : p[k];
+        m[k] = k == n ? m0 : m[k];
+        r[k] = k == n ? r0 : r[k];
+      }
+    }
   }
   const int sm = unit_byte<3>(quad_max(am)), sr = unit_byte<4>(quad_max(ar));
   if (i >= e.n) return;

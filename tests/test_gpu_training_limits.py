@@ -1,0 +1,104 @@
+"""Token embedding, AdamW over many tensors and gradient norm on the GPU: values and calls at the edge of what they take.
+
+A moment held in 8 bits is one of the two codes around it, so off by less than the gap between them: 1/8 of it for the
+first moment (3 mantissa bits), 1/16 for the root of the second (4)."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+F32 = lambda x: float(np.float32(x))
+
+
+def _draw(shape, seed, std=1.0, dtype=None):
+    import torch
+    g = torch.Generator(device="cuda:0").manual_seed(seed)
+    return (std * torch.randn(shape, device="cuda:0", generator=g)).to(dtype or torch.float32)
+
+
+def _both(n, seed, **kw):
+    """A state with 32-bit and one with 8-bit moments, of the same parameter."""
+    from paper_2605_21442_amd import AdamWTensors
+    p = _draw(n, seed, 0.5)
+    return [AdamWTensors([p.clone()], state_bits=bits, betas=(F32(0.9), F32(0.95)), **kw) for bits in (32, 8)]
+
+
+# powers of two, in blocks of 32 elements, of gradients whose square overflows fp32 (the last ones' code would round to
+# infinity) or is subnormal in it
+HUGE, TINY = [64, 65, 70, 90, 120, 126, 127, 127], [-63, -64, -66, -68, -70]
+
+
+def _blocks(exponents, seed):
+    import torch
+    g = torch.Generator(device="cuda:0").manual_seed(seed)
+    x = 1 + 0.99 * torch.rand(len(exponents), 32, device="cuda:0", generator=g)
+    x[-1] = 1.99
+    x = x * torch.tensor([2.0 ** e for e in exponents], dtype=torch.float64, device="cuda:0")[:, None]
+    x[:, ::3] *= -1
+    return x.reshape(-1).float()
+
+
+@pytest.mark.parametrize("beta", [None, 0.0])
+@pytest.mark.parametrize("scaled", [False, True])
+def test_8_bit_step_with_gradients_whose_square_overflows(scaled, beta):
+    # the parameter of lce_adamw_step, which takes no update where the second moment overflows, and moments that stay finite
+    import torch
+    g = _blocks(HUGE, 1)
+    n = g.numel()
+    assert torch.isfinite(g).all()
+    wide, narrow = _both(n, 2, lr=F32(1e-2), weight_decay=F32(0.1))
+    if beta is not None:
+        for o in (wide, narrow):
+            o.groups[0]["betas"] = (beta, beta)
+    b1, b2 = wide.groups[0]["betas"]
+    factor = torch.tensor(0.5, device="cuda:0") if scaled else None
+    for o in (wide, narrow):
+        o.step([g], grad_scale=factor)
+    assert torch.equal(narrow.params[0], wide.params[0]) and torch.isfinite(narrow.params[0]).all()
+    first, root = (x.double() for x in narrow.moments())
+    g64 = g.double() * (0.5 if scaled else 1.0)
+    m, r = (1 - b1) * g64, (1 - b2) ** 0.5 * g64.abs()
+    # the largest codes below 2^128 are held in place of what lies above them
+    m, r = m.sign() * m.abs().clamp(max=1.875 * 2.0 ** 127), r.clamp(max=1.9375 * 2.0 ** 127)
+    # (1 % for the fp32 roundings before, which are far smaller)
+    assert bool(((first - m).abs() <= 1.01 / 8 * m.abs()).all()) and bool(((root - r).abs() <= 1.01 / 16 * r).all())
+    for k in range(4):
+        narrow.step([_draw(n, 10 + k)])
+        assert torch.isfinite(narrow.params[0]).all() and all(torch.isfinite(x).all() for x in narrow.moments())
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-8])
+def test_8_bit_step_with_gradients_whose_square_is_subnormal(eps):
+    import torch
+    g = _blocks(TINY, 3)
+    wide, narrow = _both(g.numel(), 4, lr=F32(1e-2), eps=F32(eps))
+    for o in (wide, narrow):
+        o.step([g])
+    assert torch.equal(narrow.params[0], wide.params[0])
+    root, want = narrow.moments()[1].double(), wide.exp_avg_sq.double().sqrt()
+    assert bool((want > 0).all()) and bool(((root - want).abs() <= 1.01 / 16 * want).all())
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-38, 1e-31, 1e-30, 1e30, 1e31, 1e38])
+def test_8_bit_step_of_any_eps(eps):
+    # from one gradient the update is sign(g) lr, or tells eps; 8-bit states may differ from 32-bit ones by 2 ulp of the quotient
+    import torch
+    wide, narrow = _both(1000, 5, lr=F32(1e-2), eps=F32(eps), weight_decay=0.0)
+    g = _draw(1000, 6)
+    old = wide.params[0].double()
+    for o in (wide, narrow):
+        o.step([g])
+    a, b = wide.params[0].double(), narrow.params[0].double()
+    assert torch.isfinite(a).all()
+    assert bool(((a - b).abs() <= 2 * 2.0 ** -23 * (a - old).abs() + 2.0 ** -24 * a.abs() * 2).all())
+
+
+def test_8_bit_step_of_large_first_moments():
+    # (from 2^27 on the quotient is formed as lce_adamw_step forms it)
+    import torch
+    g = _blocks([20, 26, 27, 28, 30, 31, 32, 40, 60], 7)
+    wide, narrow = _both(g.numel(), 8, lr=F32(1e-2), eps=F32(1e-8))
+    for o in (wide, narrow):
+        o.step([g])
+    a, b = wide.params[0].double(), narrow.params[0].double()
+    assert bool(((a - b).abs() <= 2 * 2.0 ** -23 * 1e-2 + 2 * 2.0 ** -24 * a.abs()).all())
