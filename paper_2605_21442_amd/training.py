@@ -334,7 +334,7 @@ class AdamWTensors:
         if not native.describe(grads, self._shapes, self.device.index, t, _TENSOR.itemsize, _TENSOR.fields["grad"][1], -1,
                                _TENSOR.fields["grad_dtype"][1]):
             have = [k for k, g in enumerate(grads) if g is not None]
-            grads, t = [grads[k] for k in have], t[have]     # (the tensors without a gradient are not in the call)
+            grads, t, params = [grads[k] for k in have], t[have], [params[k] for k in have]     # (the call is of these alone)
             if any(g.shape != self._shapes[k] for g, k in zip(grads, have)):
                 raise ValueError("gradients must be shaped like their parameters")
             grads, dtypes = _dense(grads, self.device.index)
@@ -347,7 +347,7 @@ class AdamWTensors:
             B.lce_adamw_tensors_step(t.ctypes.data, len(t), opts, len(opts), self.state_bits,
                                      grad_scale.data_ptr() if grad_scale is not None else 0,
                                      self._seed_of(step) if seed is None else seed, _stream(self.device))
-        native.changed(params)                 # a graph that saved a parameter before refuses its backward now
+        native.changed(params)                 # a graph that saved one of them before refuses its backward now
         self.step_count = step
 
     def moments(self) -> tuple[torch.Tensor, torch.Tensor]:

@@ -29,6 +29,7 @@ class OnGpu:
 
         self.calls, self.param = [], lambda *shape: torch.zeros(*shape).as_subclass(Param)
         monkeypatch.setattr(TR, "_native", lambda: here)
+        monkeypatch.setattr(TR, "_dense", lambda grads, dev: ([g.contiguous() for g in grads], [TR._DTYPES[g.dtype] for g in grads]))
         monkeypatch.setattr(TR, "_stream", lambda dev: 0)
         monkeypatch.setattr(TR, "_on", lambda dev: TR._HERE)
         monkeypatch.setattr(TR.B, "lce_adamw_tensors_step",
@@ -144,3 +145,23 @@ def test_a_step_follows_the_state_where_it_was_moved(on_gpu, bits):
     assert len(on_gpu.calls) == done
     opt.step(gs)
     addresses_are_the_states()
+
+
+def test_only_the_tensors_of_the_call_count_as_changed(on_gpu):
+    # a graph that saved a parameter without a gradient in this step can still be run backward
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    a, b = on_gpu.param(4), torch.nn.Parameter(on_gpu.param(4))
+    opt = AdamWTensors([a, b])
+    x = torch.ones(4, requires_grad=True)
+    loss = (b * x).sum()
+    versions = [a._version, b._version]
+    opt.step([torch.ones(4), None])
+    assert [a._version, b._version] == [versions[0] + 1, versions[1]]
+    loss.backward()
+    opt.step([None, None])
+    assert [a._version, b._version] == [versions[0] + 1, versions[1]]
+    loss = (b * x).sum()
+    opt.step([torch.ones(4), torch.ones(4)])
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
