@@ -251,6 +251,7 @@ class AdamWTensors:
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("parameters overlap (is one given twice?)")
         self.device, self.state_bits, self.seed, self.step_count = dev, state_bits, int(seed), 0
+        self.missed = np.zeros(len(self.params), dtype=np.int64)       # steps that each tensor had no gradient in
         self.offsets, total = [], 0
         for p in self.params:
             self.offsets.append(total)
@@ -313,11 +314,12 @@ class AdamWTensors:
 
     def step(self, grads=None, grad_scale: torch.Tensor | None = None, seed: int | None = None) -> None:
         """One update. ``grads``: a gradient (bf16 or fp32, shaped like its tensor) or None per parameter, by default
-        the parameters' ``.grad``; a tensor without one is left as it is, moments included. ``grad_scale``: an fp32
-        GPU scalar that multiplies every gradient first (``grad_norm``'s factor); where it is not finite, nothing
-        changes but ``step_count``. ``seed``: 32 bits for the rounding of 8-bit moments, by default from the
-        state's seed and the step. A step captured into a graph keeps the count, the rates and the seed that it
-        was captured with in every replay."""
+        the parameters' ``.grad``; a tensor without one is left as it is, moments included, and its bias correction goes by
+        the steps that it took part in (``step_count - missed``). ``grad_scale``: an fp32 GPU scalar that multiplies every
+        gradient first (``grad_norm``'s factor); where it is not finite, nothing changes but ``step_count``: the host does
+        not know, and the bias correction of later steps counts that one. ``seed``: 32 bits for the rounding of 8-bit
+        moments, by default from the state's seed and the step. A step captured into a graph keeps the count, the rates
+        and the seed that it was captured with in every replay."""
         params = self.params
         native = _native()
         if len(params) != len(self._table) or not native.stand_at(params, self._table, _TENSOR.itemsize,
@@ -330,10 +332,10 @@ class AdamWTensors:
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1
                                        or grad_scale.device != self.device):
             raise ValueError("grad_scale must be a one-element float32 tensor on the parameters' device")
-        t = self._table.copy()
+        t, out = self._table.copy(), []
         if not native.describe(grads, self._shapes, self.device.index, t, _TENSOR.itemsize, _TENSOR.fields["grad"][1], -1,
                                _TENSOR.fields["grad_dtype"][1]):
-            have = [k for k, g in enumerate(grads) if g is not None]
+            have, out = [k for k, g in enumerate(grads) if g is not None], [k for k, g in enumerate(grads) if g is None]
             grads, t, params = [grads[k] for k in have], t[have], [params[k] for k in have]     # (the call is of these alone)
             if any(g.shape != self._shapes[k] for g, k in zip(grads, have)):
                 raise ValueError("gradients must be shaped like their parameters")
@@ -341,14 +343,22 @@ class AdamWTensors:
             t["grad"] = [g.data_ptr() for g in grads]
             t["grad_dtype"] = dtypes
         step = self.step_count + 1
-        opts = (B.LceAdamW * len(self.groups))(*(
-            B.adamw(g["lr"], g["betas"][0], g["betas"][1], g["eps"], g["weight_decay"], step) for g in self.groups))
+        # the constants' rows: the groups, or each group at each of its tensors' step counts
+        rows = [(k, 0) for k in range(len(self.groups))]
+        late = np.delete(self.missed, out) if out else self.missed
+        if late.any():
+            pairs, row = np.unique(np.stack((t["group"], late)), axis=1, return_inverse=True)
+            rows, t["group"] = pairs.T.tolist(), row.reshape(-1)
+        opts = (B.LceAdamW * len(rows))(*(
+            B.adamw(g["lr"], g["betas"][0], g["betas"][1], g["eps"], g["weight_decay"], step - late)
+            for g, late in ((self.groups[k], late) for k, late in rows)))
         with _on(self.device):
             B.lce_adamw_tensors_step(t.ctypes.data, len(t), opts, len(opts), self.state_bits,
                                      grad_scale.data_ptr() if grad_scale is not None else 0,
                                      self._seed_of(step) if seed is None else seed, _stream(self.device))
         native.changed(params)                 # a graph that saved one of them before refuses its backward now
         self.step_count = step
+        self.missed[out] += 1
 
     def moments(self) -> tuple[torch.Tensor, torch.Tensor]:
         """(first moment, root of the second), flat and exactly what the 8-bit state stands for, as bf16
@@ -365,8 +375,8 @@ class AdamWTensors:
 
     def state_dict(self) -> dict:
         """State for checkpointing (tensors are shared, not copied)."""
-        sd = {"step": self.step_count, "seed": self.seed, "state_bits": self.state_bits, "groups": [dict(g) for g in self.groups],
-              "exp_avg": self.exp_avg, "master": self.master}
+        sd = {"step": self.step_count, "missed": self.missed.tolist(), "seed": self.seed,
+              "state_bits": self.state_bits, "groups": [dict(g) for g in self.groups], "exp_avg": self.exp_avg, "master": self.master}
         return sd | ({"exp_avg_sq": self.exp_avg_sq} if self.state_bits == 32
                      else {"exp_avg_root": self.exp_avg_root, "units": self.units})
 
@@ -379,6 +389,9 @@ class AdamWTensors:
             raise ValueError("master-weight setting differs from the checkpoint")
         if len(sd.get("groups", self.groups)) != len(self.groups):
             raise ValueError("the checkpoint has another number of groups")
+        missed = np.array(sd.get("missed", [0] * len(self.params)), dtype=np.int64)
+        if missed.shape != self.missed.shape:
+            raise ValueError("the checkpoint has another number of tensors")
         names += ["master"] if self.master is not None else []
         for n in names:
             own = getattr(self, n)
@@ -386,7 +399,7 @@ class AdamWTensors:
                 raise ValueError(f"{n} is {tuple(sd[n].shape)} {sd[n].dtype} in the checkpoint, {tuple(own.shape)} {own.dtype} here")
         for n in names:
             getattr(self, n).copy_(sd[n])
-        self.step_count = int(sd["step"])
+        self.step_count, self.missed = int(sd["step"]), missed
         self.seed = int(sd.get("seed", self.seed))
         for g, x in zip(self.groups, sd.get("groups", [])):
             g.update(x)

@@ -102,3 +102,33 @@ def test_8_bit_step_of_large_first_moments():
         o.step([g])
     a, b = wide.params[0].double(), narrow.params[0].double()
     assert bool(((a - b).abs() <= 2 * 2.0 ** -23 * 1e-2 + 2 * 2.0 ** -24 * a.abs()).all())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_tensor_whose_gradients_come_late_takes_adamws_first_steps(bits):
+    # a thousand steps without a gradient: its moments are zero and its bias correction is that of the first step
+    import torch
+    from oracle import adamw_oracle as AO
+    from paper_2605_21442_amd import AdamWTensors
+    lr = F32(1e-3)
+    ps = [_draw(70, 1), _draw(300, 2)]
+    start = ps[1].double().cpu().numpy()
+    opt = AdamWTensors(ps, lr=lr, betas=(F32(0.9), F32(0.999)), weight_decay=0.0, state_bits=bits)
+    for _ in range(1000):
+        opt.step([ps[0], None])
+    assert torch.equal(ps[1].double().cpu(), torch.from_numpy(start))
+    theta, m, v = start, np.zeros(300), np.zeros(300)
+    for t in (1, 2, 3):
+        g = _draw(300, 10 + t)
+        opt.step([ps[0], g])
+        if bits == 8 and t > 1:          # from the state that the last step left
+            o = opt.offsets[1]
+            theta = before
+            m, v = first[o:o + 300], root[o:o + 300] ** 2
+        theta, m, v = AO.adamw_step(theta, g.double().cpu().numpy(), m, v, lr=lr, beta1=F32(0.9), beta2=F32(0.999), eps=F32(1e-8),
+                                    weight_decay=0.0, step=t)
+        before = ps[1].double().cpu().numpy()
+        if bits == 8:
+            first, root = (x.double().cpu().numpy() for x in opt.moments())
+        # fp32 roundings: the parameter's own, and a few of an update of at most about 10 lr
+        assert np.all(np.abs(before - theta) <= t * 2.0 ** -24 * np.abs(theta) * 1.01 + t * 1e-5 * lr)

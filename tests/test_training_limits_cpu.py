@@ -165,3 +165,42 @@ def test_only_the_tensors_of_the_call_count_as_changed(on_gpu):
     opt.step([torch.ones(4), torch.ones(4)])
     with pytest.raises(RuntimeError, match="inplace"):
         loss.backward()
+
+
+def test_bias_correction_goes_by_the_steps_that_a_tensor_took_part_in(on_gpu):
+    import copy
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    make = lambda: AdamWTensors([dict(params=[on_gpu.param(4), on_gpu.param(5)]), dict(params=[on_gpu.param(6)], lr=0.5),
+                                 dict(params=[on_gpu.param(3)], lr=0.25)])
+    opt = make()
+    gs = [torch.ones(4), torch.ones(5), torch.ones(6), torch.ones(3)]
+
+    def taken(*have):
+        """{tensor size: (rate, step)} of one step with these gradients."""
+        opt.step([g if k in have else None for k, g in enumerate(gs)])
+        t, opts, _ = on_gpu.calls[-1]
+        return {int(r["n"]): (opts[r["group"]]["lr"], opts[r["group"]]["step"]) for r in t}
+
+    a, b, c = (float(np.float32(x)) for x in (1e-3, 0.5, 0.25))
+    assert taken(0, 1, 2, 3) == {4: (a, 1), 5: (a, 1), 6: (b, 1), 3: (c, 1)}
+    assert taken(0, 2) == {4: (a, 2), 6: (b, 2)}
+    assert taken(0) == {4: (a, 3)}
+    assert taken() == {} and opt.step_count == 4
+    assert taken(0, 1, 2, 3) == {4: (a, 4), 5: (a, 2), 6: (b, 3), 3: (c, 2)}
+    assert opt.missed.tolist() == [1, 3, 2, 3]
+    state = copy.deepcopy(opt.state_dict())
+    assert taken(1, 3) == {5: (a, 3), 3: (c, 3)}
+    opt = make()
+    opt.load_state_dict(state)
+    assert taken(1, 2) == {5: (a, 3), 6: (b, 4)}
+    del state["missed"]                                # a checkpoint that does not say: every tensor took part
+    opt = make()
+    opt.load_state_dict(state)
+    assert taken(0, 1, 2, 3) == {4: (a, 6), 5: (a, 6), 6: (b, 6), 3: (c, 6)}
+    with pytest.raises(ValueError, match="number of tensors"):
+        opt.load_state_dict(dict(state, missed=[0, 0]))
+    before = opt.missed.copy(), opt.step_count
+    with pytest.raises(ValueError):
+        opt.step([gs[0], None, gs[1], None])           # refused: no count moves
+    assert (opt.missed == before[0]).all() and opt.step_count == before[1]
