@@ -213,7 +213,7 @@ _BLOCK = 32      # elements of a block of the 8-bit moments
 
 class AdamWTensors:
     """AdamW over many tensors at once (lce_adamw_tensors_step). ``params`` are contiguous bf16 or fp32 GPU tensors
-    that do not overlap, or groups of them: dicts with "params" and any of lr, betas, eps and weight_decay, which
+    that do not overlap, or groups of them: dicts with "params" (tensors, or one) and any of lr, betas, eps and weight_decay, which
     ``groups`` holds and a schedule may change between steps. ``master_weights`` keeps fp32 copies of the bf16 tensors.
 
     The state is flat: tensor i stands at ``offsets[i]`` of ``exp_avg``, ``exp_avg_sq`` and ``master``, in whole blocks
@@ -226,6 +226,8 @@ class AdamWTensors:
                  master_weights: bool = False, state_bits: int = 32, seed: int = 0):
         if state_bits not in (32, 8):
             raise ValueError(f"state_bits must be 32 or 8, got {state_bits}")
+        if isinstance(params, torch.Tensor):
+            raise TypeError("params must be a list of tensors or of groups, not a tensor (its rows would be taken for parameters)")
         params = list(params)
         groups = params if params and isinstance(params[0], dict) else [{"params": params}]
         self.params, self.groups, at = [], [], []
@@ -236,7 +238,7 @@ class AdamWTensors:
             opts = dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay)
             opts.update({o: x for o, x in g.items() if o != "params"})
             self.groups.append(opts)
-            members = list(g["params"])
+            members = [g["params"]] if isinstance(g["params"], torch.Tensor) else list(g["params"])
             self.params += members
             at += [k] * len(members)
         if not self.params:

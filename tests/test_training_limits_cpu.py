@@ -204,3 +204,13 @@ def test_bias_correction_goes_by_the_steps_that_a_tensor_took_part_in(on_gpu):
     with pytest.raises(ValueError):
         opt.step([gs[0], None, gs[1], None])           # refused: no count moves
     assert (opt.missed == before[0]).all() and opt.step_count == before[1]
+
+
+def test_a_bare_tensor_is_not_taken_apart(on_gpu):
+    # list() of a matrix gives views of its rows, which have no gradients of their own
+    from paper_2605_21442_amd import AdamWTensors
+    w, b = on_gpu.param(6, 4), on_gpu.param(3)
+    with pytest.raises(TypeError, match="rows"):
+        AdamWTensors(w)
+    opt = AdamWTensors([dict(params=w, lr=0.5), dict(params=[b])])
+    assert len(opt.params) == 2 and opt.params[0] is w and opt.params[1] is b and opt.groups[0]["lr"] == 0.5
