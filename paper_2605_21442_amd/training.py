@@ -378,12 +378,14 @@ class AdamWTensors:
     def state_dict(self) -> dict:
         """State for checkpointing (tensors are shared, not copied)."""
         sd = {"step": self.step_count, "missed": self.missed.tolist(), "seed": self.seed,
-              "state_bits": self.state_bits, "groups": [dict(g) for g in self.groups], "exp_avg": self.exp_avg, "master": self.master}
+              "state_bits": self.state_bits, "groups": [dict(g) for g in self.groups], "exp_avg": self.exp_avg, "master": self.master,
+              "shapes": [tuple(s) for s in self._shapes], "group_of": self._table["group"].tolist()}
         return sd | ({"exp_avg_sq": self.exp_avg_sq} if self.state_bits == 32
                      else {"exp_avg_root": self.exp_avg_root, "units": self.units})
 
     def load_state_dict(self, sd: dict) -> None:
-        """Restore a state_dict: moments (and master copies) are copied into this state's tensors."""
+        """Restore a state_dict: moments (and master copies) are copied into this state's tensors. The tensors must be those
+        of the checkpoint in its order: other shapes or another split into groups are refused."""
         names = ["exp_avg", "exp_avg_sq"] if self.state_bits == 32 else ["exp_avg", "exp_avg_root", "units"]
         if any(n not in sd for n in names) or sd.get("state_bits", self.state_bits) != self.state_bits:
             raise ValueError(f"the checkpoint does not hold {self.state_bits}-bit moments")
@@ -391,6 +393,9 @@ class AdamWTensors:
             raise ValueError("master-weight setting differs from the checkpoint")
         if len(sd.get("groups", self.groups)) != len(self.groups):
             raise ValueError("the checkpoint has another number of groups")
+        own = self._shapes, self._table["group"].tolist()
+        if [tuple(s) for s in sd.get("shapes", own[0])] != own[0] or list(sd.get("group_of", own[1])) != own[1]:
+            raise ValueError("the checkpoint is of tensors of other shapes, or in another order or other groups")
         missed = np.array(sd.get("missed", [0] * len(self.params)), dtype=np.int64)
         if missed.shape != self.missed.shape:
             raise ValueError("the checkpoint has another number of tensors")

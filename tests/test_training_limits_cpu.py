@@ -214,3 +214,27 @@ def test_a_bare_tensor_is_not_taken_apart(on_gpu):
         AdamWTensors(w)
     opt = AdamWTensors([dict(params=w, lr=0.5), dict(params=[b])])
     assert len(opt.params) == 2 and opt.params[0] is w and opt.params[1] is b and opt.groups[0]["lr"] == 0.5
+
+
+def test_a_checkpoint_of_other_tensors_is_refused(on_gpu):
+    # sizes of the same padded total, in another order or other groups: each tensor would get another one's moments
+    import copy
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    make = lambda *shapes, cut=1, **kw: AdamWTensors([dict(params=[on_gpu.param(*s) for s in part]) for part in (shapes[:cut], shapes[cut:])],
+                                                     **kw)
+    for kw in (dict(), dict(state_bits=8), dict(master_weights=True)):
+        a = make((3, 5), (40,), (2, 7), **kw)
+        a.exp_avg.fill_(3)
+        state = copy.deepcopy(a.state_dict())
+        for other in (make((40,), (3, 5), (2, 7), **kw), make((2, 7), (40,), (3, 5), **kw), make((5, 3), (40,), (2, 7), **kw),
+                      make((3, 5), (41,), (2, 7), **kw), make((3, 5), (40,), (2, 7), cut=2, **kw)):
+            assert other.exp_avg.shape == a.exp_avg.shape
+            with pytest.raises(ValueError, match="other"):
+                other.load_state_dict(state)
+            assert not other.exp_avg.any() and other.step_count == 0
+        same = make((3, 5), (40,), (2, 7), **kw)
+        same.load_state_dict(state)
+        assert torch.equal(same.exp_avg, a.exp_avg)
+        same = make((40,), (3, 5), (2, 7), **kw)
+        same.load_state_dict({k: v for k, v in state.items() if k not in ("shapes", "group_of")})     # one that does not say
