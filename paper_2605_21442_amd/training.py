@@ -396,7 +396,7 @@ class AdamWTensors:
         own = self._shapes, self._table["group"].tolist()
         if [tuple(s) for s in sd.get("shapes", own[0])] != own[0] or list(sd.get("group_of", own[1])) != own[1]:
             raise ValueError("the checkpoint is of tensors of other shapes, or in another order or other groups")
-        missed = np.array(sd.get("missed", [0] * len(self.params)), dtype=np.int64)
+        step, missed = int(sd["step"]), np.array(sd.get("missed", [0] * len(self.params)), dtype=np.int64)
         if missed.shape != self.missed.shape:
             raise ValueError("the checkpoint has another number of tensors")
         names += ["master"] if self.master is not None else []
@@ -406,7 +406,7 @@ class AdamWTensors:
                 raise ValueError(f"{n} is {tuple(sd[n].shape)} {sd[n].dtype} in the checkpoint, {tuple(own.shape)} {own.dtype} here")
         for n in names:
             getattr(self, n).copy_(sd[n])
-        self.step_count, self.missed = int(sd["step"]), missed
+        self.step_count, self.missed = step, missed
         self.seed = int(sd.get("seed", self.seed))
         for g, x in zip(self.groups, sd.get("groups", [])):
             g.update(x)

@@ -238,3 +238,14 @@ def test_a_checkpoint_of_other_tensors_is_refused(on_gpu):
         assert torch.equal(same.exp_avg, a.exp_avg)
         same = make((40,), (3, 5), (2, 7), **kw)
         same.load_state_dict({k: v for k, v in state.items() if k not in ("shapes", "group_of")})     # one that does not say
+
+
+def test_a_checkpoint_without_its_step_changes_nothing(on_gpu):
+    from paper_2605_21442_amd import AdamWTensors
+    a, b = AdamWTensors([on_gpu.param(4)]), AdamWTensors([on_gpu.param(4)])
+    a.exp_avg.fill_(1)
+    state = a.state_dict()
+    del state["step"]
+    with pytest.raises(KeyError):
+        b.load_state_dict(state)
+    assert not b.exp_avg.any()
