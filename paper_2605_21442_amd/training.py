@@ -59,6 +59,8 @@ def _rows(x: torch.Tensor, name: str) -> tuple[torch.Tensor, int]:
         raise TypeError(f"{name} must be bfloat16 or float32, got {x.dtype}")
     if not x.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
+    if x.is_neg():                   # its memory holds the values with the other sign, also after contiguous()
+        x = x.resolve_neg()
     x2 = x.reshape(-1, x.shape[-1]) if x.dim() != 2 else x
     if not _rows_usable(tuple(x2.shape), x2.stride(), x2.data_ptr()):
         x2 = x2.contiguous()
@@ -110,7 +112,8 @@ def embedding_backward(ids: torch.Tensor, grad_out: torch.Tensor, v: int, scale:
         raise ValueError(f"ids has {t.numel()} entries for {n} rows of grad_out")
     if accumulate_into is not None:
         dw = accumulate_into
-        if tuple(dw.shape) != (v, d) or not dw.is_contiguous() or dw.device != x.device or dw.dtype not in (x.dtype, torch.float32):
+        if (tuple(dw.shape) != (v, d) or not dw.is_contiguous() or dw.is_neg() or dw.device != x.device
+                or dw.dtype not in (x.dtype, torch.float32)):
             raise ValueError(f"accumulate_into must be a contiguous [{v}, {d}] tensor of grad_out's dtype or float32 on its device")
     else:
         dw_dtype = x.dtype if dw_dtype is None else dw_dtype
@@ -247,7 +250,7 @@ class AdamWTensors:
         for p in self.params:
             if p.dtype not in _DTYPES:
                 raise TypeError(f"parameters must be bfloat16 or float32, got {p.dtype}")
-            if not p.is_cuda or p.device != dev or not p.is_contiguous():
+            if not p.is_cuda or p.device != dev or not p.is_contiguous() or p.is_neg():
                 raise ValueError("parameters must be contiguous GPU tensors on one device, since they are updated in place")
         spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()) for p in self.params if p.numel())
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
@@ -332,7 +335,7 @@ class AdamWTensors:
         if len(grads) != len(params):
             raise ValueError(f"{len(grads)} gradients for {len(params)} parameters")
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1
-                                       or grad_scale.device != self.device):
+                                       or grad_scale.device != self.device or grad_scale.is_neg()):
             raise ValueError("grad_scale must be a one-element float32 tensor on the parameters' device")
         t, out = self._table.copy(), []
         if not native.describe(grads, self._shapes, self.device.index, t, _TENSOR.itemsize, _TENSOR.fields["grad"][1], -1,

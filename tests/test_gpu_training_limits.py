@@ -132,3 +132,29 @@ def test_a_tensor_whose_gradients_come_late_takes_adamws_first_steps(bits):
             first, root = (x.double().cpu().numpy() for x in opt.moments())
         # fp32 roundings: the parameter's own, and a few of an update of at most about 10 lr
         assert np.all(np.abs(before - theta) <= t * 2.0 ** -24 * np.abs(theta) * 1.01 + t * 1e-5 * lr)
+
+
+def test_tensors_with_a_negative_bit():
+    # (the imaginary part of a conjugate has one: its memory holds the other sign)
+    import torch
+    from paper_2605_21442_amd import AdamWTensors, grad_norm, token_embedding
+    from paper_2605_21442_amd.training import embedding_backward, embedding_forward
+    ids = torch.tensor([1, 3, 1, 0], device="cuda:0")
+    w, x = _draw((5, 16), 1), _draw((4, 16), 2)
+    neg = lambda t: torch._neg_view(-t)                # the same values
+    assert neg(w).is_neg() and torch.equal(neg(w), w)
+    assert torch.equal(embedding_forward(ids, neg(w))[0], w[ids])
+    assert torch.equal(embedding_backward(ids, neg(x), 5), embedding_backward(ids, x, 5))
+    part = torch.complex(w, -w).conj().imag            # (and its columns lie apart)
+    assert part.is_neg() and torch.equal(token_embedding(ids, part), w[ids])
+    with pytest.raises(ValueError):
+        embedding_backward(ids, x, 5, accumulate_into=neg(w))
+    with pytest.raises(ValueError):
+        AdamWTensors([neg(w)])
+    ps = [w.clone(), w.clone()]
+    for p, g in zip(ps, (neg(_draw((5, 16), 3)), _draw((5, 16), 3))):
+        opt = AdamWTensors([p])
+        opt.step([g], grad_scale=torch.ones(1, device="cuda:0"))
+        with pytest.raises(ValueError):
+            opt.step([g], grad_scale=neg(torch.ones(1, device="cuda:0")))
+    assert torch.equal(*ps) and grad_norm([neg(x)])[0].item() == grad_norm([x])[0].item()
