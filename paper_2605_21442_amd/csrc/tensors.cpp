@@ -14,6 +14,12 @@
 
 namespace {
 
+// Whether all of a contiguous tensor lies within its storage, which may have been resized (to nothing, for offloading).
+bool fits_storage(const at::Tensor& t) {
+  return t.numel() == 0 ||
+         (t.storage_offset() + t.numel()) * static_cast<int64_t>(t.element_size()) <= static_cast<int64_t>(t.storage().nbytes());
+}
+
 // The tensor behind an entry of a list, if it is plain memory of the device (index, or -1 for the host): strided,
 // contiguous, bf16 or fp32. dtype: lce_dtype_t.
 const at::Tensor* plain(PyObject* o, int64_t device, int32_t* dtype) {
@@ -24,7 +30,7 @@ const at::Tensor* plain(PyObject* o, int64_t device, int32_t* dtype) {
   else if (t.scalar_type() == at::kFloat) *dtype = 1;
   else return nullptr;
   if (device < 0 ? !t.is_cpu() : !t.is_cuda() || t.get_device() != device) return nullptr;
-  if (!t.has_storage() || !t.is_contiguous() || t.is_neg()) return nullptr;
+  if (!t.has_storage() || !t.is_contiguous() || t.is_neg() || !fits_storage(t)) return nullptr;
   return &t;
 }
 
@@ -85,8 +91,7 @@ PyObject* describe(PyObject*, PyObject* args) {
 bool lies_whole(const at::Tensor& t, int64_t count, int32_t dtype) {
   if (!t.defined() || t.layout() != at::kStrided || t.scalar_type() != (dtype == 2 ? at::kByte : dtype == 1 ? at::kFloat : at::kBFloat16))
     return false;
-  return t.has_storage() && t.is_contiguous() && !t.is_neg() && t.numel() == count &&
-         (t.storage_offset() + count) * static_cast<int64_t>(t.element_size()) <= static_cast<int64_t>(t.storage().nbytes());
+  return t.has_storage() && t.is_contiguous() && !t.is_neg() && t.numel() == count && fits_storage(t);
 }
 
 // stand_at(tensors, table, row_bytes, o_data, o_n = -1, o_dtype = -1) -> bool: whether each tensor still has the address

@@ -181,6 +181,16 @@ def _dense(grads: list, dev_index: int | None) -> tuple[list, list]:
     return [g.resolve_neg().contiguous() for g in grads], [_DTYPES[g.dtype] for g in grads]
 
 
+def _list_dense(grads: list, dtypes: list, t: np.ndarray, data: str, dtype: str) -> None:
+    """The tensors of ``_dense`` into a table that holds their sizes. The library takes a gradient without an address for
+    zeros: one without memory of its own is refused."""
+    t[data] = [g.data_ptr() for g in grads]
+    t[dtype] = dtypes
+    if ((t[data] == 0) & (t["n"] > 0)).any() or not _native().stand_at(grads, t, t.dtype.itemsize,
+                                                                       *(t.dtype.fields[k][1] for k in (data, "n", dtype))):
+        raise TypeError("gradients must have memory of their own (a wrapper, or a tensor whose storage was resized, has not)")
+
+
 def grad_norm(grads, max_norm: float = math.inf) -> tuple[torch.Tensor, torch.Tensor]:
     """(norm, factor), fp32 scalars on the device, from lce_grad_norm: the norm of all tensors of ``grads``
     together (None entries are left out) and ``min(1, max_norm / (norm + 1e-6))``, for ``AdamWTensors.step``'s
@@ -193,9 +203,8 @@ def grad_norm(grads, max_norm: float = math.inf) -> tuple[torch.Tensor, torch.Te
         if not grads:
             raise ValueError("no gradients")
         t = np.zeros(len(grads), dtype=_GRAD)
-        t["data"] = [g.data_ptr() for g in grads]
         t["n"] = [g.numel() for g in grads]
-        t["dtype"] = dtypes
+        _list_dense(grads, dtypes, t, "data", "dtype")
     dev = grads[0].device
     addr = t.ctypes.data
     nbytes = B.lce_grad_norm_workspace_size(addr, len(grads))
@@ -345,8 +354,7 @@ class AdamWTensors:
             if any(g.shape != self._shapes[k] for g, k in zip(grads, have)):
                 raise ValueError("gradients must be shaped like their parameters")
             grads, dtypes = _dense(grads, self.device.index)
-            t["grad"] = [g.data_ptr() for g in grads]
-            t["grad_dtype"] = dtypes
+            _list_dense(grads, dtypes, t, "grad", "grad_dtype")
         step = self.step_count + 1
         # the constants' rows: the groups, or each group at each of its tensors' step counts
         rows = [(k, 0) for k in range(len(self.groups))]

@@ -249,3 +249,37 @@ def test_a_checkpoint_without_its_step_changes_nothing(on_gpu):
     with pytest.raises(KeyError):
         b.load_state_dict(state)
     assert not b.exp_avg.any()
+
+
+def test_a_gradient_without_memory_is_not_taken_for_zeros(on_gpu):
+    import torch
+    from paper_2605_21442_amd import AdamWTensors, training as TR
+
+    class Wrapper(torch.Tensor):
+        @staticmethod
+        def __new__(cls, t):
+            return torch.Tensor._make_wrapper_subclass(cls, t.shape, dtype=t.dtype, device="cuda:0")
+
+        @classmethod
+        def __torch_dispatch__(cls, func, types, args=(), kwargs=None):
+            raise AssertionError(func)
+
+    freed, cut = torch.ones(3), torch.ones(8)
+    freed.untyped_storage().resize_(0)
+    for bad in (Wrapper(torch.ones(3)), freed):
+        with pytest.raises(TypeError, match="memory"):
+            AdamWTensors([on_gpu.param(4), on_gpu.param(3)]).step([torch.ones(4), bad])
+        with pytest.raises(TypeError, match="memory"):
+            TR.grad_norm([torch.ones(4), bad])
+        assert not on_gpu.calls
+    AdamWTensors([on_gpu.param(4), on_gpu.param(0), on_gpu.param(2)]).step([torch.ones(4), torch.ones(0), None])
+    assert len(on_gpu.calls) == 1
+    t = np.zeros(1, dtype=TABLE)
+    fills = lambda x: TR._native().describe([x], None, -1, t, TABLE.itemsize, 8, 0, 20)
+    assert fills(cut) and fills(cut[5:]) and fills(torch.zeros(0))
+    assert freed.numel() == 3 and not fills(freed)
+    tail = cut[5:]
+    cut.untyped_storage().resize_(24)                  # six of its elements
+    assert not fills(cut) and not fills(tail) and fills(cut[:6])
+    with pytest.raises(TypeError, match="memory"):
+        AdamWTensors([on_gpu.param(8)]).step([cut])
