@@ -15,7 +15,9 @@ __all__ = ["linear_cross_entropy", "LinearCrossEntropy", "AdamWState", "linear_k
 
 def __getattr__(name):
     if name in __all__:
-        from . import autograd, training
-        value = globals()[name] = getattr(autograd if hasattr(autograd, name) else training, name)
+        from . import autograd as home
+        if not hasattr(home, name):          # (the loss needs nothing of the other operators, nor numpy)
+            from . import training as home
+        value = globals()[name] = getattr(home, name)
         return value
     raise AttributeError(name)

@@ -283,3 +283,20 @@ def test_a_gradient_without_memory_is_not_taken_for_zeros(on_gpu):
     assert not fills(cut) and not fills(tail) and fills(cut[:6])
     with pytest.raises(TypeError, match="memory"):
         AdamWTensors([on_gpu.param(8)]).step([cut])
+
+
+def test_the_losss_names_do_not_need_the_other_operators():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = ("import sys, paper_2605_21442_amd as p\n"
+            "sys.modules['paper_2605_21442_amd.training'] = None\n"          # importing it fails
+            "assert p.linear_cross_entropy and p.AdamWState and p.LinearKD\n"
+            "try: p.grad_norm\n"
+            "except ImportError: pass\n"
+            "else: raise AssertionError('imported')\n"
+            "del sys.modules['paper_2605_21442_amd.training']\n"
+            "assert all(getattr(p, n) for n in p.__all__)\n")
+    res = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=120)
+    assert res.returncode == 0, res.stderr
