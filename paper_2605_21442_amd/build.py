@@ -4,13 +4,14 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "lce.hip")
 OUT = os.path.join(PKG, "liblce.so")
 TENSORS_SRC = os.path.join(PKG, "csrc", "tensors.cpp")
-TENSORS_OUT = os.path.join(PKG, "_tensors.so")
+TENSORS_OUT = os.path.join(PKG, "_tensors" + sysconfig.get_config_var("EXT_SUFFIX"))   # (no other interpreter loads it)
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CXX = os.environ.get("CXX", "g++")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
@@ -36,8 +37,6 @@ def _run(cmd: list[str], out: str, verbose: bool) -> None:
 
 def build_tensors(verbose: bool = False) -> str:
     """The host extension, against the installed torch (whose libraries are in the process before it is loaded)."""
-    import sysconfig
-
     import torch
     from torch.utils import cpp_extension
 

@@ -8,6 +8,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/version.h>
 
 #include <cstdint>
 #include <cstring>
@@ -169,4 +170,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__tensors() { return PyModule_Create(&module); }
+// torch_version: whose tensors' layout the module was compiled for
+PyMODINIT_FUNC PyInit__tensors() {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) != 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}

@@ -31,11 +31,13 @@ def _native():
     """The extension that reads lists of tensors (csrc/tensors.cpp); like liblce.so it is needed, not replaced."""
     global _ext
     if _ext is None:
+        how = "; run `python -c 'import __graft_entry__ as g; g.build()'` from the repository root"
         try:
             from . import _tensors
         except ImportError as e:
-            raise RuntimeError("_tensors.so is not built for this Python and torch; run `python -c 'import __graft_entry__ as "
-                               "g; g.build()'` from the repository root") from e
+            raise RuntimeError("the extension _tensors is not built for this Python and torch" + how) from e
+        if not torch.__version__.startswith(_tensors.torch_version):
+            raise RuntimeError(f"the extension _tensors was built for torch {_tensors.torch_version}, not {torch.__version__}" + how)
         _ext = _tensors
     return _ext
 

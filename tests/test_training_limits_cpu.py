@@ -300,3 +300,16 @@ def test_the_losss_names_do_not_need_the_other_operators():
             "assert all(getattr(p, n) for n in p.__all__)\n")
     res = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=120)
     assert res.returncode == 0, res.stderr
+
+
+def test_an_extension_of_another_interpreter_or_torch_is_not_used(monkeypatch):
+    # it reads torch's own structures: one built for others would read something else
+    import sysconfig
+    import torch
+    from paper_2605_21442_amd import build, training as TR
+    assert build.TENSORS_OUT.endswith("_tensors" + sysconfig.get_config_var("EXT_SUFFIX"))
+    assert TR._native().__file__ == build.TENSORS_OUT
+    monkeypatch.setattr(TR, "_ext", None)
+    monkeypatch.setattr(torch, "__version__", "1.2.3+rocm")
+    with pytest.raises(RuntimeError, match="built for torch"):
+        TR._native()
