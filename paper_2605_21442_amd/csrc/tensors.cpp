@@ -161,10 +161,25 @@ PyObject* current_stream(PyObject*, PyObject* device) {
   }
 }
 
+// negative(tensor), dual(tensor) -> bool: whether its memory holds its values with the other sign; whether it has a forward-mode
+// tangent. (Through Python 0.3 and 0.8 us of a call that takes 11.)
+PyObject* negative(PyObject*, PyObject* o) { return PyBool_FromLong(THPVariable_Check(o) && THPVariable_Unpack(o).is_neg()); }
+
+PyObject* dual(PyObject*, PyObject* o) {
+  try {
+    return PyBool_FromLong(THPVariable_Check(o) && THPVariable_Unpack(o)._fw_grad(0).defined());
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
 PyMethodDef methods[] = {{"describe", describe, METH_VARARGS, nullptr},
                          {"stand_at", stand_at, METH_VARARGS, nullptr},
                          {"changed", changed, METH_O, nullptr},
                          {"current_stream", current_stream, METH_O, nullptr},
+                         {"negative", negative, METH_O, nullptr},
+                         {"dual", dual, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -14,7 +14,6 @@ import math
 
 import numpy as np
 import torch
-from torch.autograd.forward_ad import unpack_dual
 from torch.autograd.function import once_differentiable
 from torch.autograd.graph import increment_version
 
@@ -61,7 +60,7 @@ def _rows(x: torch.Tensor, name: str) -> tuple[torch.Tensor, int]:
         raise TypeError(f"{name} must be bfloat16 or float32, got {x.dtype}")
     if not x.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
-    if x.is_neg():                   # its memory holds the values with the other sign, also after contiguous()
+    if _native().negative(x):        # its memory holds the values with the other sign, also after contiguous()
         x = x.resolve_neg()
     x2 = x.reshape(-1, x.shape[-1]) if x.dim() != 2 else x
     if not _rows_usable(tuple(x2.shape), x2.stride(), x2.data_ptr()):
@@ -161,7 +160,7 @@ def token_embedding(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0,
     """``scale * weight[ids]``: the token embedding, with a gradient for the weight [V, D] (bf16 or fp32). Tokens
     of ``padding_idx`` give no gradient. An id outside the vocabulary gives a row of zeros and no gradient
     (``embedding_forward`` also reports it). Forward-mode derivatives are refused."""
-    if not (weight.requires_grad and torch.is_grad_enabled()) and unpack_dual(weight).tangent is None:
+    if not (weight.requires_grad and torch.is_grad_enabled()) and not _native().dual(weight):
         return embedding_forward(ids, weight, scale, padding_idx, want_status=False)[0]
     return TokenEmbedding.apply(ids, weight, scale, padding_idx)
 
