@@ -158,3 +158,52 @@ def test_tensors_with_a_negative_bit():
         with pytest.raises(ValueError):
             opt.step([g], grad_scale=neg(torch.ones(1, device="cuda:0")))
     assert torch.equal(*ps) and grad_norm([neg(x)])[0].item() == grad_norm([x])[0].item()
+
+
+def test_fp32_output_and_gradient_that_pass_the_caches_by():
+    # an output and a fresh dW larger than the caches keep, in the wider type
+    import torch
+    from paper_2605_21442_amd.training import embedding_backward, embedding_forward
+    n, d, v = 16411, 4104, 140001
+    print(f"case n={n} d={d} v={v} f32", flush=True)
+    w = _draw((v, 256), 1).repeat(1, 17)[:, :d].contiguous()
+    ids = torch.from_numpy(np.random.default_rng(2).zipf(1.2, n + 1) % v).to("cuda:0")[1:]
+    out, status = embedding_forward(ids, w, 3.0)
+    assert int(status.item()) == 0 and torch.equal(out, w[ids] * 3.0)
+    ref = torch.zeros(v, d, dtype=torch.float64, device="cuda:0").index_add_(0, ids, out.double())
+    mag = torch.zeros(v, d, dtype=torch.float64, device="cuda:0").index_add_(0, ids, out.double().abs())
+    k = torch.bincount(ids, minlength=v)[:, None]
+    tol = (k + 3) * 2.0 ** -24 * 1.01 * mag
+    dw = embedding_backward(ids, out, v)
+    assert bool(((dw.double() - ref).abs() <= tol).all()) and not dw[k[:, 0] == 0].any()
+    x = out.bfloat16()
+    wide = embedding_backward(ids, x, v, dw_dtype=torch.float32)
+    assert bool(((wide.double() - ref).abs() <= tol + 2.0 ** -8 * 1.01 * mag).all()) and not wide[k[:, 0] == 0].any()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_large_tensor_at_an_odd_place_matches_float64(bits):
+    # no array but the moments at a multiple of 16 bytes, and a size that no round divides
+    import torch
+    from oracle import adamw_oracle as AO
+    from paper_2605_21442_amd import AdamWTensors
+    n = 3_000_017
+    flat, grads = _draw(n + 9, 1, 0.5, torch.bfloat16), _draw(n + 9, 2, 0.1)
+    p, g = flat[3:3 + n], grads[1:1 + n]
+    around = flat[:3].clone(), flat[3 + n:].clone()
+    start = p.double().cpu().numpy()
+    opt = AdamWTensors([p], state_bits=bits, lr=F32(1e-2), betas=(F32(0.9), F32(0.95)), weight_decay=F32(0.1))
+    opt.step([g])
+    theta, m, v = AO.adamw_step(start, g.double().cpu().numpy(), np.zeros(n), np.zeros(n), lr=F32(1e-2), beta1=F32(0.9),
+                                beta2=F32(0.95), eps=F32(1e-8), weight_decay=F32(0.1), step=1)
+    # one rounding to bf16, and a few fp32 ones of the parameter and of the update
+    tol = 4 * 2.0 ** -24 * np.abs(theta) + 1e-5 * 1e-2
+    assert np.all(np.abs(p.double().cpu().numpy() - theta) <= tol + 2.0 ** -8 * (np.abs(theta) + tol))
+    assert torch.equal(flat[:3], around[0]) and torch.equal(flat[3 + n:], around[1])
+    if bits == 32:
+        assert np.all(np.abs(opt.exp_avg[:n].double().cpu().numpy() - m) <= 2.0 ** -23 * np.abs(m))
+        assert np.all(np.abs(opt.exp_avg_sq[:n].double().cpu().numpy() - v) <= 2.0 ** -22 * np.abs(v) + 1e-44)
+    else:
+        first = opt.moments()[0][:n].double().cpu().numpy()
+        top = np.abs(m).max()
+        assert np.all(np.abs(first - m) <= 1.01 / 8 * np.abs(m) + top * 2.0 ** -16)      # (small ones: steps of the block's unit)
