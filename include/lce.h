@@ -405,8 +405,9 @@ lce_status_t lce_kd_forward_backward(const lce_kd_problem_t* p,
  *   dW[v]  = scale * sum of dOut[n] over the tokens with id_n = v, id_n != padding_idx
  *
  * A vocabulary shard (lce_shard_t's fields: W holds ids [v_begin, v_begin + v) of v_total) looks up
- * and gathers only its own ids; the outputs of all shards sum to the whole. out and dW are dense; dW is
- * at most 2^35 bytes.
+ * and gathers only its own ids; the outputs of all shards sum to the whole. out and dW are dense; V D elements
+ * of dW's type are at most 2^35 bytes, and N V is at most 2^53 for the gradient, whose sort takes time in
+ * proportion to N V from 2^18 ids on.
  * Elements are bf16 or fp32 (dtype: W, out and dOut; dw_dtype: dW, which may also be fp32 for a bf16
  * model). Sums run in fp32 in an order that the ids alone fix, and are rounded once.
  */

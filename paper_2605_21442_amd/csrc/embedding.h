@@ -529,6 +529,10 @@ struct EmbedPlan {
   size_t o_sorted, o_starts, o_parts, bytes;
 };
 
+// Of the gradient: every bucket of the sort looks at every id, and there are v / 1024 buckets from 2^18 ids on, so its time grows
+// with n v. At 2^53 it is near 15 s (2^43 looks at 0.4 ns a CU); without a limit the largest n and v would take half an hour.
+constexpr int64_t kMostLooks = (int64_t)1 << 53;
+
 inline bool known_dtype(int32_t t) { return t == LCE_DTYPE_BF16 || t == LCE_DTYPE_F32; }
 
 lce_status_t make_embed_plan(const lce_embedding_t* p, EmbedPlan* pl) {
@@ -634,6 +638,7 @@ lce_status_t lce_embedding_workspace_size(const lce_embedding_t* p, size_t* bwd_
   EmbedPlan pl;
   const lce_status_t st = make_embed_plan(p, &pl);
   if (st != LCE_OK) return st;
+  if (p->n * p->v > kMostLooks) return LCE_ERR_SHAPE;
   if (!bwd_bytes) return LCE_ERR_NULL;
   *bwd_bytes = pl.bytes;
   return LCE_OK;
@@ -659,6 +664,7 @@ lce_status_t lce_embedding_backward(const lce_embedding_t* p, const void* ids, c
   EmbedPlan pl;
   const lce_status_t st = make_embed_plan(p, &pl);
   if (st != LCE_OK) return st;
+  if (p->n * p->v > kMostLooks) return LCE_ERR_SHAPE;
   if (!dW || !workspace || (p->n > 0 && (!ids || !dOut))) return LCE_ERR_NULL;
   if (((uintptr_t)ids & (p->id_bytes - 1)) != 0 || !aligned16(dOut) || !aligned16(dW) || ((uintptr_t)workspace & 255) != 0) return LCE_ERR_ALIGN;
   if (workspace_bytes < pl.bytes) return LCE_ERR_WORKSPACE;

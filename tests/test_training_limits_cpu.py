@@ -313,3 +313,19 @@ def test_an_extension_of_another_interpreter_or_torch_is_not_used(monkeypatch):
     monkeypatch.setattr(torch, "__version__", "1.2.3+rocm")
     with pytest.raises(RuntimeError, match="built for torch"):
         TR._native()
+
+
+def test_a_gradient_whose_sort_would_hold_the_gpu_is_refused():
+    # (nothing is launched: the sizes are refused, or the workspace is missing)
+    from paper_2605_21442_amd import binding as B
+    at = 0x100000
+    for n, v, ok in [((1 << 30) - 1, (1 << 30) - 1, False), (1 << 24, (1 << 29) + 1, False), (1 << 24, 1 << 29, True),
+                     ((1 << 23) - 1, (1 << 30) - 1, True), ((1 << 30) - 1, 1 << 18, True), (1 << 20, (1 << 30) - 1, True)]:
+        p = B.embedding(n, 8, v)
+        for call in (lambda: B.lce_embedding_workspace_size(p), lambda: B.lce_embedding_backward(p, at, 2 * at, 3 * at, 0, 0, 0)):
+            try:
+                call()
+                code = 0
+            except B.LceError as e:
+                code = e.code
+            assert code == (B.LCE_ERR_SHAPE if not ok else code) and (not ok or code in (0, B.LCE_ERR_NULL)), (n, v, code)
