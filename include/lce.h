@@ -443,9 +443,9 @@ typedef struct lce_embedding {
 lce_status_t lce_embedding_workspace_size(const lce_embedding_t* p, size_t* bwd_bytes);
 
 /*
- * Lookup (ids need the alignment of their type only). out [N, D], overwritten; the row of an id that W does not hold is 0. dev_status [1] int32
- * or NULL: overwritten with status bits (LCE_STATUS_ID_OUT_OF_RANGE). p->flags, dw_dtype and ld_x
- * are checked but not used.
+ * Lookup (ids need the alignment of their type only). out [N, D], overwritten; the row of an id that W does not
+ * hold is 0. dev_status [1] int32 or NULL: overwritten with status bits (LCE_STATUS_ID_OUT_OF_RANGE).
+ * p->flags, dw_dtype and ld_x are checked but not used.
  */
 lce_status_t lce_embedding_forward(const lce_embedding_t* p, const void* W, const void* ids, void* out,
                                    int32_t* dev_status, void* stream);
@@ -465,8 +465,8 @@ lce_status_t lce_embedding_backward(const lce_embedding_t* p, const void* ids, c
  * is n contiguous elements.
  *   param          bf16 or fp32, updated in place
  *   grad           bf16 or fp32, or NULL for a zero gradient
- *   exp_avg, exp_avg_sq, units: the moments, updated in place (16-byte aligned, units 2). state_bits 32: fp32 [n]
- *                  each, units NULL. state_bits 8: one byte per element, exp_avg_sq holding the root of
+ *   exp_avg, exp_avg_sq, units: the moments, updated in place (16-byte aligned, units 2). state_bits 32: fp32
+ *                  [n] each, units NULL. state_bits 8: one byte per element, exp_avg_sq holding the root of
  *                  the second moment, and two unit bytes for each 32 elements (the last block may be
  *                  short), [ceil(n / 32)][2]. Zero bytes throughout are the state before the first step.
  *   master         fp32 [n] or NULL: as W_master of lce_adamw_step, for a bf16 param

@@ -10,17 +10,17 @@
 namespace {
 
 // ---------------------------------------------------------------------------------------------
-// Sort. Ids are dealt to `nb` (a power of two) buckets by their low bits, so that the frequent ids, which lie
-// close together in a vocabulary ordered by frequency, fall into different buckets. One workgroup of 16 waves
-// serves a bucket on its own: it reads all N ids, counts those of lower buckets (which is where its bucket
-// starts) and, per wave and id, those of its own; a scan over (id, wave) gives every wave the place of its first
-// token of every id, at which it then puts its tokens. A wave owns consecutive tokens, so the order within an id is
-// the tokens'. No workgroup waits for another, and counts do not depend on an order. A wave lists its tokens of the
-// bucket in LDS as it counts them, so only one with more than the list holds walks the ids twice.
-// 709 / 4096 / 16384 / 65070 tokens: 6.2 / 7.2 / 10.2 / 30 us. Short batches are bound by the chain of loads, barriers and the
-// scan; long ones by the vector instructions of the walk (every bucket looks at every id) in the bucket of the
-// most frequent id, 0.3 to 0.5 us per 1000 tokens. (Ranks by one ballot per bit for every group of 64 tokens, without
-// the lists: 22 us for 16384 tokens; ids loaded one group at a time: 30.)
+// Sort. Ids are dealt to `nb` (a power of two) buckets by their low bits, so that the frequent ids, which lie close
+// together in a vocabulary ordered by frequency, fall into different buckets. One workgroup of 16 waves serves a
+// bucket on its own: it reads all N ids, counts those of lower buckets (which is where its bucket starts) and, per
+// wave and id, those of its own; a scan over (id, wave) gives every wave the place of its first token of every id, at
+// which it then puts its tokens. A wave owns consecutive tokens, so the order within an id is the tokens'. No
+// workgroup waits for another, and counts do not depend on an order. A wave lists its tokens of the bucket in LDS as
+// it counts them, so only one with more than the list holds walks the ids twice. 709 / 4096 / 16384 / 65070 tokens:
+// 6.2 / 7.2 / 10.2 / 30 us. Short batches are bound by the chain of loads, barriers and the scan; long ones by the
+// vector instructions of the walk (every bucket looks at every id) in the bucket of the most frequent id, 0.3 to 0.5
+// us per 1000 tokens. (Ranks by one ballot per bit for every group of 64 tokens, without the lists: 22 us for 16384
+// tokens; ids loaded one group at a time: 30.)
 // ---------------------------------------------------------------------------------------------
 constexpr int kSortWaves = 16;
 constexpr int kSortIds = 1024;     // most ids of a bucket, one per thread in the scan
@@ -162,12 +162,12 @@ __global__ __launch_bounds__(1024) void k_embed_sort(EmbedRows e, int nb_log2, i
 }
 
 // ---------------------------------------------------------------------------------------------
-// Lookup: a workgroup writes 8192 consecutive elements of out, a thread 8 of every 2048 of them, so that the rows of four
-// pieces are in flight and the stores go in the order of the addresses. kOnce: the stores pass the L2 and the 256 MB MALL by.
-// An output that fits there is better kept, for the layer that reads it next: W cold, 16384 tokens of 4096 (134 MB)
-// looked up and then read take 77 us kept and 88 passed by, 2048 (17 MB) 19 and 22; one that does not fit is better
-// passed by, 32768 (268 MB) 167 and 159. (Lookups of nothing else in a row, whose rows of W then stay in the MALL: 134 MB
-// 37 and 29.5 us, 235 MB 70 and 49.5.)
+// Lookup: a workgroup writes 8192 consecutive elements of out, a thread 8 of every 2048 of them, so that the rows of
+// four pieces are in flight and the stores go in the order of the addresses. kOnce: the stores pass the L2 and the
+// 256 MB MALL by. An output that fits there is better kept, for the layer that reads it next: W cold, 16384 tokens of
+// 4096 (134 MB) looked up and then read take 77 us kept and 88 passed by, 2048 (17 MB) 19 and 22; one that does not
+// fit is better passed by, 32768 (268 MB) 167 and 159. (Lookups of nothing else in a row, whose rows of W then stay
+// in the MALL: 134 MB 37 and 29.5 us, 235 MB 70 and 49.5.)
 // ---------------------------------------------------------------------------------------------
 // 8 elements: as they lie in memory (so that a load is only issued where it stands), and as fp32
 template <typename T> struct Row8;
@@ -177,7 +177,10 @@ template <> struct Row8<uint16_t> {
   static __device__ __forceinline__ void unpack(const Raw& r, float x[8]) {
     const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
+    for (int k = 0; k < 4; ++k) {
+      x[2 * k] = __uint_as_float(w[k] << 16);
+      x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+    }
   }
   template <bool kOnce = false>      // written once: not kept in the L2
   static __device__ __forceinline__ void store(uint16_t* p, const float x[8]) {
@@ -260,13 +263,13 @@ __global__ __launch_bounds__(256) void k_embed_lookup(EmbedIds e, int64_t v_tota
 __global__ void k_embed_clear_status(int* status) { *status = 0; }
 
 // ---------------------------------------------------------------------------------------------
-// Gradient: the sorted tokens are cut into chunks of `per` consecutive ones, and a wave takes a chunk's tokens at
-// 512 columns (8 per lane), eight rows of dOut in flight. An id whose tokens lie in one chunk is finished there. One
-// that reaches over a chunk's edge leaves an fp32 sum per chunk, in the chunk's slot 0 where it goes on from the chunk
-// before and in slot 1 where it starts, and k_embed_join adds these in the order of the chunks. So a frequent id
-// is spread over many waves, and the order of all sums follows from the ids and N alone.
-// Bound by memory: 4096 tokens added to a 128256 x 8192 dW 21.5 us (5.5 TB/s), 32768 to a 152064 x 3584 dW 64 us (4.6); one
-// workgroup per id, the simplest form, took 700 us for the former: the most frequent id's tokens came one after the other.
+// Gradient: the sorted tokens are cut into chunks of `per` consecutive ones, and a wave takes a chunk's tokens at 512
+// columns (8 per lane), eight rows of dOut in flight. An id whose tokens lie in one chunk is finished there. One that
+// reaches over a chunk's edge leaves an fp32 sum per chunk, in the chunk's slot 0 where it goes on from the chunk
+// before and in slot 1 where it starts, and k_embed_join adds these in the order of the chunks. So a frequent id is
+// spread over many waves, and the order of all sums follows from the ids and N alone. Bound by memory: 4096 tokens
+// added to a 128256 x 8192 dW 21.5 us (5.5 TB/s), 32768 to a 152064 x 3584 dW 64 us (4.6); one workgroup per id, the
+// simplest form, took 700 us for the former: the most frequent id's tokens came one after the other.
 // ---------------------------------------------------------------------------------------------
 constexpr int kGradCols = 512;     // columns of a wave
 
@@ -274,7 +277,9 @@ struct EmbedSorted {
   const int2* pairs;               // (row of W, token), by id
   const int* starts;               // first pair of each id, bucket by bucket
   int nb_log2, rows;
-  __device__ __forceinline__ int64_t slot(int r) const { return (int64_t)(r & ((1 << nb_log2) - 1)) * rows + (r >> nb_log2); }
+  __device__ __forceinline__ int64_t slot(int r) const {
+    return (int64_t)(r & ((1 << nb_log2) - 1)) * rows + (r >> nb_log2);
+  }
   __device__ __forceinline__ int count() const { return starts[(int64_t)rows << nb_log2]; }
 };
 
@@ -350,8 +355,8 @@ __global__ __launch_bounds__(256) void k_embed_grad(EmbedSorted s, const T* __re
 }
 
 // The rows of a fresh dW without a token, in the order of the addresses: 16 KB of dW per workgroup, 16 bytes of each
-// 4 KB per thread. (All rows of 128256 x 4096 bf16 in pieces of 16 KB: 6.7 TB/s, as a fill without a look at the rows; of 4 KB, whose
-// two loads come before the one store, 5.1; whole rows by wave 5.5 to 6.0.)
+// 4 KB per thread. (All rows of 128256 x 4096 bf16 in pieces of 16 KB: 6.7 TB/s, as a fill without a look at the
+// rows; of 4 KB, whose two loads come before the one store, 5.1; whole rows by wave 5.5 to 6.0.)
 constexpr int kFillAhead = 4;
 constexpr int64_t kFillBytes = 256 * 16 * kFillAhead;
 
@@ -373,10 +378,11 @@ __device__ __forceinline__ void embed_fill(const EmbedSorted& s, int64_t block, 
     if (empty[k]) store16_padded(o + 4096 * k, i32x4_t{0, 0, 0, 0});
 }
 
-// The sums of ids that several chunks share: one workgroup per chunk and 512 columns, which has work where an id starts in
-// the chunk and reaches past its end. Wave w adds every fourth of the id's chunks from the w-th on, four loads in flight; the
-// waves' sums are added in order. Behind these workgroups come those of embed_fill: here they have the 32 waves a
-// CU holds, which the registers of k_embed_grad would halve (709 tokens, 128256 x 2048: 100 us there).
+// The sums of ids that several chunks share: one workgroup per chunk and 512 columns, which has work where an id
+// starts in the chunk and reaches past its end. Wave w adds every fourth of the id's chunks from the w-th on, four
+// loads in flight; the waves' sums are added in order. Behind these workgroups come those of embed_fill: here they
+// have the 32 waves a CU holds, which the registers of k_embed_grad would halve (709 tokens, 128256 x 2048: 100 us
+// there).
 template <typename TW, bool kAdd>
 __global__ __launch_bounds__(256) void k_embed_join(EmbedSorted s, int v, int d, int per, int slices, int64_t join_blocks,
                                                     float scale, TW* __restrict__ dw, const float* __restrict__ parts) {
@@ -426,13 +432,13 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedSorted s, int v, int d,
 }
 
 // ---------------------------------------------------------------------------------------------
-// Gradient of few tokens, without a sort: a workgroup per token and 512 columns lists the tokens of its token's id, in order,
-// from a look at all ids, and goes on if its own is the first of them. Its four waves add a quarter of the rows each, eight
-// in flight, and the quarters are added in order. A fresh dW is zeroed by a launch before.
-// Two launches (one where dW is added to) instead of three, whose latencies are all that few tokens cost. Added, replayed:
-// 256 tokens of 512 columns 3.9 us against 13.0 by the sort, 1024 of 2048 9.4 against 14.8; 4096 workgroups are the
-// limit (1024 of 4096 26 against 16) and 1024 tokens too, for the batch whose tokens are all one id (1024 of 512 23.5 against
-// 15.5, 2048 45 against 19).
+// Gradient of few tokens, without a sort: a workgroup per token and 512 columns lists the tokens of its token's id,
+// in order, from a look at all ids, and goes on if its own is the first of them. Its four waves add a quarter of the
+// rows each, eight in flight, and the quarters are added in order. A fresh dW is zeroed by a launch before. Two
+// launches (one where dW is added to) instead of three, whose latencies are all that few tokens cost. Added,
+// replayed: 256 tokens of 512 columns 3.9 us against 13.0 by the sort, 1024 of 2048 9.4 against 14.8; 4096 workgroups
+// are the limit (1024 of 4096 26 against 16) and 1024 tokens too, for the batch whose tokens are all one id (1024 of
+// 512 23.5 against 15.5, 2048 45 against 19).
 // ---------------------------------------------------------------------------------------------
 constexpr int kFewTokens = 1024;
 
@@ -509,7 +515,8 @@ __global__ __launch_bounds__(256) void k_embed_few(EmbedRows e, const T* __restr
   grad_store<TW, kAdd>(o, old, sum, scale);
 }
 
-// kOnce: past the caches, which a dW larger than they are would only empty of dOut (16384 tokens, 128256 x 4096: 213 -> 202 us)
+// kOnce: past the caches, which a dW larger than they are would only empty of dOut (16384 tokens, 128256 x 4096: 213
+// -> 202 us)
 template <bool kOnce>
 __global__ __launch_bounds__(256) void k_embed_zero(char* __restrict__ dw, int64_t bytes) {
   const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 16;
@@ -529,8 +536,9 @@ struct EmbedPlan {
   size_t o_sorted, o_starts, o_parts, bytes;
 };
 
-// Of the gradient: every bucket of the sort looks at every id, and there are v / 1024 buckets from 2^18 ids on, so its time grows
-// with n v. At 2^53 it is near 15 s (2^43 looks at 0.4 ns a CU); without a limit the largest n and v would take half an hour.
+// Of the gradient: every bucket of the sort looks at every id, and there are v / 1024 buckets from 2^18 ids on, so
+// its time grows with n v. At 2^53 it is near 15 s (2^43 looks at 0.4 ns a CU); without a limit the largest n and v
+// would take half an hour.
 constexpr int64_t kMostLooks = (int64_t)1 << 53;
 
 inline bool known_dtype(int32_t t) { return t == LCE_DTYPE_BF16 || t == LCE_DTYPE_F32; }
@@ -548,7 +556,8 @@ lce_status_t make_embed_plan(const lce_embedding_t* p, EmbedPlan* pl) {
     return LCE_ERR_SHAPE;
   pl->ldw = p->ld_w ? p->ld_w : p->d;
   pl->ldx = p->ld_x ? p->ld_x : p->d;
-  if (pl->ldw < p->d || pl->ldx < p->d || pl->ldw >= (int64_t)1 << 30 || pl->ldx >= (int64_t)1 << 30) return LCE_ERR_SHAPE;
+  if (pl->ldw < p->d || pl->ldx < p->d || pl->ldw >= (int64_t)1 << 30 || pl->ldx >= (int64_t)1 << 30)
+    return LCE_ERR_SHAPE;
   if (pl->ldw % 8 != 0 || pl->ldx % 8 != 0) return LCE_ERR_ALIGN;
   // a launch takes fewer than 2^32 threads, and zeroes 4 KB of dW with 256 of them
   if ((uint64_t)p->v * p->d * (p->dw_dtype == LCE_DTYPE_F32 ? 4 : 2) > (uint64_t)1 << 35) return LCE_ERR_SHAPE;
@@ -561,12 +570,14 @@ lce_status_t make_embed_plan(const lce_embedding_t* p, EmbedPlan* pl) {
   size_t cur = 0;
   pl->o_sorted = take(cur, 8 * (size_t)p->n);
   pl->o_starts = take(cur, 4 * (((size_t)pl->rows << pl->nb_log2) + 1));
-  // tokens of a chunk: 8 to 64, for 4096 waves (16 per CU, each with eight rows' loads in flight), and in narrow rows no
-  // fewer than keep the chunks of a frequent id few for the join, which takes 16 of them a step as a wave takes 8 rows
-  // (65070 tokens of 88: 58 us with 16); more where there would be more than 4096 chunks, whose sums bound the workspace
+  // tokens of a chunk: 8 to 64, for 4096 waves (16 per CU, each with eight rows' loads in flight), and in narrow rows
+  // no fewer than keep the chunks of a frequent id few for the join, which takes 16 of them a step as a wave takes 8
+  // rows (65070 tokens of 88: 58 us with 16); more where there would be more than 4096 chunks, whose sums bound the
+  // workspace
   pl->slices = (int)((p->d + kGradCols - 1) / kGradCols);
   pl->per = 8;
-  while (pl->per < 64 && (p->n * pl->slices > (int64_t)4096 * pl->per || p->n > (int64_t)16 * pl->per * pl->per)) pl->per *= 2;
+  while (pl->per < 64 && (p->n * pl->slices > (int64_t)4096 * pl->per || p->n > (int64_t)16 * pl->per * pl->per))
+    pl->per *= 2;
   while (p->n > (int64_t)4096 * pl->per) pl->per *= 2;
   pl->chunks = (p->n + pl->per - 1) / pl->per;
   pl->o_parts = take(cur, 8 * (size_t)pl->chunks * p->d);
@@ -579,8 +590,9 @@ void launch_lookup(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, c
                    int32_t* status) {
   const int64_t blocks = (p->n * (p->d / 8) + 1023) / 1024;
   const bool kept = p->n * p->d * (int64_t)sizeof(T) <= kKeptBytes;
-  L(K_EMBED_LOOKUP, kept ? k_embed_lookup<T, false> : k_embed_lookup<T, true>, dim3((unsigned)std::min<int64_t>(blocks, 1 << 20)), dim3(256), e, pl.v_total,
-    (const T*)W, pl.ldw, (int)p->d, p->scale, (T*)out, status);
+  L(K_EMBED_LOOKUP, kept ? k_embed_lookup<T, false> : k_embed_lookup<T, true>,
+    dim3((unsigned)std::min<int64_t>(blocks, 1 << 20)), dim3(256), e, pl.v_total, (const T*)W, pl.ldw, (int)p->d,
+    p->scale, (T*)out, status);
 }
 
 void launch_zero(Launcher& L, void* dw, int64_t bytes) {
@@ -610,7 +622,8 @@ inline bool few_tokens(const lce_embedding_t* p, const EmbedPlan& pl) {
 }
 
 template <typename T, typename TW, bool kAdd>
-void launch_embed_few(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedRows& e, const void* dout, void* dw) {
+void launch_embed_few(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedRows& e, const void* dout,
+                      void* dw) {
   const int64_t bytes = p->v * p->d * (int64_t)sizeof(TW);
   if (!kAdd) launch_zero(L, dw, bytes);
   L(K_EMBED_GRAD, p->id_bytes == 8 ? k_embed_few<T, TW, kAdd, 8> : k_embed_few<T, TW, kAdd, 4>,
@@ -618,7 +631,8 @@ void launch_embed_few(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl
 }
 
 template <typename T, typename TW>
-void launch_embed_few(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedRows& e, const void* dout, void* dw) {
+void launch_embed_few(Launcher& L, const lce_embedding_t* p, const EmbedPlan& pl, const EmbedRows& e, const void* dout,
+                      void* dw) {
   if (p->flags & LCE_FLAG_ACCUMULATE_DW) launch_embed_few<T, TW, true>(L, p, pl, e, dout, dw);
   else launch_embed_few<T, TW, false>(L, p, pl, e, dout, dw);
 }
@@ -666,7 +680,8 @@ lce_status_t lce_embedding_backward(const lce_embedding_t* p, const void* ids, c
   if (st != LCE_OK) return st;
   if (p->n * p->v > kMostLooks) return LCE_ERR_SHAPE;
   if (!dW || !workspace || (p->n > 0 && (!ids || !dOut))) return LCE_ERR_NULL;
-  if (((uintptr_t)ids & (p->id_bytes - 1)) != 0 || !aligned16(dOut) || !aligned16(dW) || ((uintptr_t)workspace & 255) != 0) return LCE_ERR_ALIGN;
+  if (((uintptr_t)ids & (p->id_bytes - 1)) != 0 || !aligned16(dOut) || !aligned16(dW) || ((uintptr_t)workspace & 255) != 0)
+    return LCE_ERR_ALIGN;
   if (workspace_bytes < pl.bytes) return LCE_ERR_WORKSPACE;
   Launcher L{(hipStream_t)stream};
   char* ws = (char*)workspace;

@@ -2,11 +2,12 @@
 // behind its launcher. A launch serves dozens of tensors, whose addresses travel in its arguments: nothing
 // is copied to the device beforehand, so a call can be captured and its table needs no storage.
 //
-// All of it is bound by memory on a whole model (1.2e9 bf16 elements): the 32-bit step with an fp32 master copy moves
-// 28 bytes an element in 5.6 to 5.9 ms (5.9 to 6.2 TB/s), the 8-bit step without 10.1 bytes in 2.55 to 2.63 ms (4.8 TB/s; its
-// vector instructions alone would take 2.0), the values of the 8-bit moments 6.1 bytes in 1.3 ms (5.7), the norm 2 bytes in
-// 0.40 ms (6.1). Hundreds of small tensors are bound by the launches' ramps (224 adapter tensors, 11.3e6 elements: 64 us in 3
-// launches, 4.9 TB/s; in 5 launches 74) and, in the norm, by the host (15 us of kernels and 18 a call).
+// On a whole model (1.24e9 bf16 elements, kernels alone under the tracer) the 32-bit step with an fp32 master copy
+// moves 28 bytes an element in 5.7 ms (6.1 TB/s), the values of the 8-bit moments 6.1 bytes in 1.2 ms (6.2) and the
+// norm 2 bytes in 0.40 ms (6.1): bound by memory. The 8-bit step without master copy moves 10.1 bytes in 2.4 ms (5.3
+// TB/s), of which its 66 vector instructions an element alone would take 2.1. Hundreds of small tensors are bound by
+// the launches' ramps (224 adapter tensors, 11.3e6 elements: 64 us in 3 launches, 4.9 TB/s; in 5 launches 74) and, in
+// the norm, by the host (9 us of kernels and 18 a call).
 #pragma once
 
 namespace {
@@ -62,8 +63,8 @@ __device__ __forceinline__ float load_elem(const void* p, int64_t i, bool f32) {
 }
 
 // N consecutive elements from i on as fp32, and back; elements at or past n are 0 and are not touched. `wide`: the
-// tensor's address is a multiple of 16 bytes (i is a multiple of N). Both pass the L2 by: a step touches every byte once
-// (1.2e9 elements, 32-bit moments, 8192 a workgroup: 6.72 -> 6.57 ms; adapters 117 -> 107 us).
+// tensor's address is a multiple of 16 bytes (i is a multiple of N). Both pass the L2 by: a step touches every byte
+// once (1.2e9 elements, 32-bit moments, 8192 a workgroup: 6.72 -> 6.57 ms; adapters 117 -> 107 us).
 template <int N>
 __device__ __forceinline__ void load_elems(const void* p, int64_t i, int64_t n, bool f32, bool wide, float x[N]) {
   if (wide && i + N <= n) {
@@ -78,7 +79,10 @@ __device__ __forceinline__ void load_elems(const void* p, int64_t i, int64_t n, 
       typedef uint32_t Words __attribute__((ext_vector_type(N / 2)));
       const Words a = __builtin_nontemporal_load(reinterpret_cast<const Words*>((const uint16_t*)p + i));
 #pragma unroll
-      for (int h = 0; h < N / 2; ++h) { x[2 * h] = __uint_as_float(a[h] << 16); x[2 * h + 1] = __uint_as_float(a[h] & 0xFFFF0000u); }
+      for (int h = 0; h < N / 2; ++h) {
+        x[2 * h] = __uint_as_float(a[h] << 16);
+        x[2 * h + 1] = __uint_as_float(a[h] & 0xFFFF0000u);
+      }
     }
     return;
   }
@@ -92,8 +96,9 @@ __device__ __forceinline__ void store_elems(void* p, int64_t i, int64_t n, bool 
     if (f32) {
 #pragma unroll
       for (int h = 0; h < N / 4; ++h)
-        store16_padded_nt((float*)p + i + 4 * h, i32x4_t{(int)__float_as_uint(x[4 * h]), (int)__float_as_uint(x[4 * h + 1]),
-                                                      (int)__float_as_uint(x[4 * h + 2]), (int)__float_as_uint(x[4 * h + 3])});
+        store16_padded_nt((float*)p + i + 4 * h,
+                          i32x4_t{(int)__float_as_uint(x[4 * h]), (int)__float_as_uint(x[4 * h + 1]),
+                                  (int)__float_as_uint(x[4 * h + 2]), (int)__float_as_uint(x[4 * h + 3])});
     } else if (N == 8) {
       store16_padded_nt((uint16_t*)p + i, i32x4_t{(int)pack_bf16x2(x[0], x[1]), (int)pack_bf16x2(x[2], x[3]),
                                                (int)pack_bf16x2(x[N - 4], x[N - 3]), (int)pack_bf16x2(x[N - 2], x[N - 1])});
@@ -138,7 +143,8 @@ __device__ __forceinline__ uint32_t dithered(float x, int s, uint32_t bits) {
 
 // byte 3 of each of four words, as one word
 __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0703u), __builtin_amdgcn_perm(b, a, 0x0C0C0703u), 0x05040100u);
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0703u), __builtin_amdgcn_perm(b, a, 0x0C0C0703u),
+                               0x05040100u);
 }
 
 // 16 random bits for each of two neighbouring elements: a multiplicative hash (Knuth, TAOCP 6.4) of the
@@ -157,8 +163,8 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
   return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));   // lanes 2 3 0 1
 }
 
-// What a byte of the first moment (a sign and a 7-bit code) and one of the root stand for. A block of NaN has its codes'
-// exponent bits all set.
+// What a byte of the first moment (a sign and a 7-bit code) and one of the root stand for. A block of NaN has its
+// codes' exponent bits all set.
 __device__ __forceinline__ float decode_first(uint32_t byte, int sm) {
   const int c = (int)(byte << 24) >> 4;           // sign, copies of it, code
   return ldexpf(__uint_as_float(((uint32_t)c & 0x87F00000u) | (sm == 255 ? 0x7FC00000u : 0u)), code_exponent<3>(sm));
@@ -177,11 +183,12 @@ __device__ __forceinline__ void decode_moments(const uint2 cm, const uint2 cr, i
   }
 }
 
-// The parameter's update of 8-bit states from the new moments: adamw_update's, but for the root and the quotient. Each is
-// the hardware's estimate (1 ulp) with one Newton step, which is the correctly rounded value but for a few in a million. The
-// compiler's own sequences, which are right for every operand, made the 8-bit step bound by the vector units (91
-// instructions an element, 3.04 ms for 1.2e9). The short form is for v = 0 or normal, eps within 2^+-100 and |m| < 2^27, so that
-// no estimate, product or quotient leaves the normal numbers (but a quotient too small to matter). Returns the root.
+// The parameter's update of 8-bit states from the new moments: adamw_update's, but for the root and the quotient.
+// Each is the hardware's estimate (1 ulp) with one Newton step, which is the correctly rounded value but for a few in
+// a million. The compiler's own sequences, which are right for every operand, made the 8-bit step bound by the vector
+// units (91 instructions an element; 3.04 ms for 1.2e9 where this form took 2.55). The short form is for v = 0 or
+// normal, eps within 2^+-100 and |m| < 2^27, so that no estimate, product or quotient leaves the normal numbers (but
+// a quotient too small to matter). Returns the root.
 __device__ __forceinline__ float adamw_step_near(float& p, float m, float v, const AdamWConst& c) {
 #pragma clang fp contract(off)
   p = p * c.keep;
@@ -193,13 +200,14 @@ __device__ __forceinline__ float adamw_step_near(float& p, float m, float v, con
   return root;
 }
 
-// The same for all other operands, bit for bit adamw_update's parameter: a v that overflows gives no update. The root that is
-// held is then formed from scaled terms, so that gradients that are finite leave moments that are (those in the last 1/16 and
-// 1/32 below 2^128, whose code could round to infinity, are held as the largest code there; and beta2 = 0 takes nothing of
-// an r whose square overflows). It starts from the element's values in memory: kept in registers until here, the kernel
-// had 81 to 103 of them instead of 61, and every step took 3 % longer. A tensor of such operands alone takes 2.2 times as long.
-__device__ __forceinline__ void adamw_element_far(const AdamWEntry<8>& e, const AdamWConst& c, int64_t i, float scale, bool scaled,
-                                                  int s, float& p, float& m, float& r) {
+// The same for all other operands, bit for bit adamw_update's parameter: a v that overflows gives no update. The root
+// that is held is then formed from scaled terms, so that gradients that are finite leave moments that are (those in
+// the last 1/16 and 1/32 below 2^128, whose code could round to infinity, are held as the largest code there; and
+// beta2 = 0 takes nothing of an r whose square overflows). It starts from the element's values in memory: kept in
+// registers until here, the kernel had 81 to 103 of them instead of 61, and every step took 3 % longer. A tensor of
+// such operands alone takes 2.2 times as long.
+__device__ __forceinline__ void adamw_element_far(const AdamWEntry<8>& e, const AdamWConst& c, int64_t i, float scale,
+                                                  bool scaled, int s, float& p, float& m, float& r) {
 #pragma clang fp contract(off)
   const float old = decode_root(((const uint8_t*)e.v)[i], s >> 8);
   float g = e.grad ? load_elem(e.grad, i, e.grad_f32) : 0.f;
@@ -219,7 +227,8 @@ __device__ __forceinline__ void adamw_element_far(const AdamWEntry<8>& e, const 
 }
 
 // 32-bit moments: 4 elements per thread and round, so that every access of a wave is contiguous.
-__device__ __forceinline__ void adamw_round32(const AdamWEntry<32>& e, const AdamWConst& c, int64_t i, float scale, bool scaled) {
+__device__ __forceinline__ void adamw_round32(const AdamWEntry<32>& e, const AdamWConst& c, int64_t i, float scale,
+                                              bool scaled) {
 #pragma clang fp contract(off)
   float p[4], g[4] = {}, m[4], v[4];
   load_elems<4>(e.m, i, e.n, true, true, m);
@@ -240,8 +249,8 @@ __device__ __forceinline__ void adamw_round32(const AdamWEntry<32>& e, const Ada
 
 // 8-bit moments: 8 elements per thread and round, four lanes to a block. Every lane of a wave comes here (the
 // blocks' maxima pass between lanes); those at or past n hold zeros.
-__device__ __forceinline__ void adamw_round8(const AdamWEntry<8>& e, const AdamWConst& c, int64_t i, float scale, bool scaled,
-                                             uint32_t seed) {
+__device__ __forceinline__ void adamw_round8(const AdamWEntry<8>& e, const AdamWConst& c, int64_t i, float scale,
+                                             bool scaled, uint32_t seed) {
 #pragma clang fp contract(off)
   float p[8] = {}, g[8] = {}, m[8] = {}, r[8] = {};
   uint8_t* units = e.units + 2 * (i / kMomentBlock);
@@ -280,7 +289,8 @@ __device__ __forceinline__ void adamw_round8(const AdamWEntry<8>& e, const AdamW
   far |= am >= 0x4D000000u;                            // 2^27
   if (far) {
     am = ar = 0;
-#pragma unroll 1                    // (the address is hidden from the compiler, which would keep one of each array in registers)
+    // (the address is hidden from the compiler, which would keep one of each array in registers)
+#pragma unroll 1
     for (int n = 0; n < 8 && i + n < e.n; ++n) {
       float p0, m0, r0;
       int64_t at = i + n;
@@ -330,7 +340,8 @@ __device__ __forceinline__ void adamw_round8(const AdamWEntry<8>& e, const AdamW
 }
 
 template <int kBits>
-__global__ __launch_bounds__(256) void k_adamw_tensors(AdamWTable<kBits> t, const float* __restrict__ grad_scale, uint32_t seed) {
+__global__ __launch_bounds__(256) void k_adamw_tensors(AdamWTable<kBits> t, const float* __restrict__ grad_scale,
+                                                       uint32_t seed) {
   const float scale = grad_scale ? *grad_scale : 1.0f;
   if (!(fabsf(scale) < INFINITY)) return;
   const AdamWEntry<kBits> e = t.e[table_entry(t.e, t.count, blockIdx.x)];
@@ -416,8 +427,8 @@ __device__ __forceinline__ double squares(const uint4 a, bool f32) {
   return lo + hi;
 }
 
-// A workgroup takes `bytes` bytes of a tensor in 16-byte pieces, eight in flight per thread; the tensor's elements before the
-// first multiple of 16 bytes and behind the last are added one by one by its first workgroup.
+// A workgroup takes `bytes` bytes of a tensor in 16-byte pieces, eight in flight per thread; the tensor's elements
+// before the first multiple of 16 bytes and behind the last are added one by one by its first workgroup.
 __global__ __launch_bounds__(256) void k_grad_squares(NormTable t, int64_t bytes, double* __restrict__ parts) {
   constexpr int kAhead = 8;
   const NormEntry e = t.e[table_entry(t.e, t.count, blockIdx.x)];
@@ -474,7 +485,8 @@ inline uintptr_t dtype_bytes(int32_t t) { return t == LCE_DTYPE_F32 ? 4 : 2; }
 
 lce_status_t check_adamw_tensor(const lce_adamw_tensor_t& t, int32_t n_groups, int32_t bits) {
   if (t.n < 0 || t.n >= kMostElems) return LCE_ERR_SHAPE;
-  if (t.reserved != 0 || t.group < 0 || t.group >= n_groups || t.place < 0 || t.place % kMomentBlock != 0) return LCE_ERR_ARG;
+  if (t.reserved != 0 || t.group < 0 || t.group >= n_groups || t.place < 0 || t.place % kMomentBlock != 0)
+    return LCE_ERR_ARG;
   if (!known_dtype(t.param_dtype) || !known_dtype(t.grad_dtype)) return LCE_ERR_UNSUPPORTED;
   if (t.n == 0) return LCE_OK;
   if (t.master && t.param_dtype != LCE_DTYPE_BF16) return LCE_ERR_ARG;
@@ -550,10 +562,11 @@ template <int kBits>
 void launch_adamw(Launcher& L, const lce_adamw_tensor_t* tensors, int64_t count, const lce_adamw_t* groups, int64_t total,
                   const float* grad_scale, uint32_t seed) {
   AdamWTable<kBits> t;
-  // elements of a workgroup. 32-bit moments: one round, so that the workgroups go through the addresses in order (1.2e9
-  // elements 5.80 ms; 2048, 4096, 8192 a workgroup: 6.24, 6.31, 6.54). 8-bit ones, which the vector units bound as much: one
-  // round (2048) to fill the card, or up to 16384 where there are more than 8192 workgroups, each of which first finds
-  // its tensor (1.2e9 elements 2.34 ms, with 2048: 2.49; 5.3e6 elements 28 us with 8192, 25 with 2048)
+  // elements of a workgroup. 32-bit moments: one round, so that the workgroups go through the addresses in order
+  // (1.2e9 elements 5.80 ms; 2048, 4096, 8192 a workgroup: 6.24, 6.31, 6.54). 8-bit ones, which the vector units
+  // bound as much: one round (2048) to fill the card, or up to 16384 where there are more than 8192 workgroups, each
+  // of which first finds its tensor (1.2e9 elements 2.34 ms against 2.49 with 2048, in one run; 5.3e6 elements 28 us
+  // with 8192, 25 with 2048)
   t.per = kBits == 8 ? 2048 : 1024;
   while (kBits == 8 && t.per < 16384 && total > (int64_t)8192 * t.per) t.per *= 2;
   int32_t group_of[kTableGroups];
@@ -661,7 +674,8 @@ lce_status_t lce_grad_norm(const lce_grad_t* grads, int64_t count, float max_nor
   for (int64_t i = 0; i < count; ++i) {
     const lce_grad_t& g = grads[i];
     for (int64_t at = 0; at < g.n; at += kNormEntryElems) {
-      const lce_grad_t part{(const char*)g.data + at * dtype_bytes(g.dtype), std::min(g.n - at, kNormEntryElems), g.dtype, 0};
+      const lce_grad_t part{(const char*)g.data + at * dtype_bytes(g.dtype), std::min(g.n - at, kNormEntryElems),
+                            g.dtype, 0};
       const int64_t nb = norm_part_blocks(part, bytes);
       if (t.count == kNormTensors || here + nb > kMostBlocks) flush();
       t.e[t.count++] = NormEntry{part.data, (uint32_t)part.n, (uint32_t)here, (uint32_t)(g.dtype == LCE_DTYPE_F32)};

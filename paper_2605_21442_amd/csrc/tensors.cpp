@@ -1,9 +1,10 @@
-// Python extension module _tensors: the host side of calls over many tensors. A model has hundreds of them, and reading each
-// one's type, device, layout, shape and address through Python takes a third of a microsecond, which for adapters is
-// longer than the GPU works (224 gradients: norm 73 us of host for 15 of kernels). Here it is a loop over the list.
+// Python extension module _tensors: the host side of calls over many tensors. A model has hundreds of them, and
+// reading each one's type, device, layout, shape and address through Python takes a third of a microsecond, which for
+// adapters is longer than the GPU works (224 gradients: norm 73 us of host for 15 of kernels). Here it is a loop over
+// the list.
 //
-// Nothing is computed and nothing is kept; tensors that need more than reading (another type or device, strides, None, a
-// subclass that is not memory) are left to the caller, who takes them one by one.
+// Nothing is computed and nothing is kept; tensors that need more than reading (another type or device, strides,
+// None, a subclass that is not memory) are left to the caller, who takes them one by one.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/core/Tensor.h>
@@ -47,10 +48,10 @@ bool has_shape(const at::Tensor& t, PyObject* shape) {
   return true;
 }
 
-// describe(tensors, shapes, device, table, row_bytes, o_data, o_n, o_dtype) -> bool
-// Writes each tensor's address (uint64 at o_data of its row of the table), element count (int64 at o_n, unless o_n < 0) and
-// type (int32 at o_dtype). shapes: None, or the shape (a tuple) that each must have. False, with the table half
-// written, where some tensor is not plain memory of the device or not of its shape.
+// describe(tensors, shapes, device, table, row_bytes, o_data, o_n, o_dtype) -> bool Writes each tensor's address
+// (uint64 at o_data of its row of the table), element count (int64 at o_n, unless o_n < 0) and type (int32 at
+// o_dtype). shapes: None, or the shape (a tuple) that each must have. False, with the table half written, where some
+// tensor is not plain memory of the device or not of its shape.
 PyObject* describe(PyObject*, PyObject* args) {
   PyObject *list, *shapes;
   Py_buffer table;
@@ -95,8 +96,8 @@ bool lies_whole(const at::Tensor& t, int64_t count, int32_t dtype) {
   return t.has_storage() && t.is_contiguous() && !t.is_neg() && t.numel() == count && fits_storage(t);
 }
 
-// stand_at(tensors, table, row_bytes, o_data, o_n = -1, o_dtype = -1) -> bool: whether each tensor still has the address
-// in its row and, with o_n and o_dtype, is still as many elements of that type without gaps.
+// stand_at(tensors, table, row_bytes, o_data, o_n = -1, o_dtype = -1) -> bool: whether each tensor still has the
+// address in its row and, with o_n and o_dtype, is still as many elements of that type without gaps.
 PyObject* stand_at(PyObject*, PyObject* args) {
   PyObject* list;
   Py_buffer table;
@@ -148,8 +149,8 @@ PyObject* changed(PyObject*, PyObject* list) {
   Py_RETURN_NONE;
 }
 
-// current_stream(device) -> int: the hipStream_t that torch works on there (0: the default stream). Through torch's Stream
-// object this takes 2 us, a sixth of a small call.
+// current_stream(device) -> int: the hipStream_t that torch works on there (0: the default stream). Through torch's
+// Stream object this takes 2 us, a sixth of a small call.
 PyObject* current_stream(PyObject*, PyObject* device) {
   const long index = PyLong_AsLong(device);
   if (index == -1 && PyErr_Occurred()) return nullptr;
@@ -161,8 +162,8 @@ PyObject* current_stream(PyObject*, PyObject* device) {
   }
 }
 
-// negative(tensor), dual(tensor) -> bool: whether its memory holds its values with the other sign; whether it has a forward-mode
-// tangent. (Through Python 0.3 and 0.8 us of a call that takes 11.)
+// negative(tensor), dual(tensor) -> bool: whether its memory holds its values with the other sign; whether it has a
+// forward-mode tangent. (Through Python 0.3 and 0.8 us of a call that takes 11.)
 PyObject* negative(PyObject*, PyObject* o) { return PyBool_FromLong(THPVariable_Check(o) && THPVariable_Unpack(o).is_neg()); }
 
 PyObject* dual(PyObject*, PyObject* o) {

@@ -158,7 +158,8 @@ class TokenEmbedding(torch.autograd.Function):
 def token_embedding(ids: torch.Tensor, weight: torch.Tensor, scale: float = 1.0,
                     padding_idx: int | None = None) -> torch.Tensor:
     """``scale * weight[ids]``: the token embedding, with a gradient for the weight [V, D] (bf16 or fp32). Tokens
-    of ``padding_idx`` give no gradient. An id outside the vocabulary gives a row of zeros and no gradient
+    of ``padding_idx`` give no gradient; one that is no id of the vocabulary, such as -1 or -100, stands for tokens whose
+    rows are zeros (it does not count from the end). An id outside the vocabulary gives a row of zeros and no gradient
     (``embedding_forward`` also reports it). Forward-mode derivatives are refused."""
     if not (weight.requires_grad and torch.is_grad_enabled()) and not _native().dual(weight):
         return embedding_forward(ids, weight, scale, padding_idx, want_status=False)[0]
