@@ -207,3 +207,33 @@ def test_a_large_tensor_at_an_odd_place_matches_float64(bits):
         first = opt.moments()[0][:n].double().cpu().numpy()
         top = np.abs(m).max()
         assert np.all(np.abs(first - m) <= 1.01 / 8 * np.abs(m) + top * 2.0 ** -16)      # (small ones: steps of the block's unit)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_state_that_was_replaced_or_offloaded_goes_on_bit_for_bit(bits):
+    import torch
+    from paper_2605_21442_amd import AdamWTensors
+    make = lambda: [_draw(s, k, 0.5, torch.bfloat16) for k, s in enumerate([(70, 9), (33,), (5000,)])]
+    ps, qs = make(), make()
+    a, b = (AdamWTensors(x, state_bits=bits, master_weights=True, seed=3) for x in (ps, qs))
+    names = ["exp_avg", "master"] + (["exp_avg_sq"] if bits == 32 else ["exp_avg_root", "units"])
+    left = []
+    for t in range(6):
+        gs = [_draw(p.shape, 10 * t + k, 0.1, torch.bfloat16) for k, p in enumerate(ps)]
+        if t % 2:                        # one gradient missing, one strided: the list that is read tensor by tensor
+            gs[1], gs[0] = None, gs[0].T.contiguous().T
+        a.step(gs)
+        b.step(gs)
+        for n in names:                  # out to the host and back into other memory; the old one holds other values
+            own = getattr(b, n)
+            left.append(own)
+            setattr(b, n, own.cpu().to("cuda:0"))
+            own.fill_(77)
+    assert all(torch.equal(x, y) for x, y in zip(ps, qs))
+    assert all(torch.equal(getattr(a, n), getattr(b, n)) for n in names)
+    assert all((x == 77).all() for x in left)
+    if bits == 8:
+        assert all(torch.equal(x, y) for x, y in zip(a.moments(), b.moments()))
+    b.exp_avg = b.exp_avg.cpu()
+    with pytest.raises(ValueError, match="exp_avg"):
+        b.step(gs)
